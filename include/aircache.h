@@ -323,6 +323,130 @@ int aircache_decode_attn_static(const aircache_shape_t *shape, const aircache_ra
 int aircache_append(const aircache_shape_t *shape, aircache_ragged_t *cache, const void *k_new,
                     const void *v_new, int32_t appended, void *cuda_stream);
 
+/* ---------------------------------------------------------------------------
+ * In front of the compression: the prompt.  (The paper takes its keys and
+ * values as given.)
+ * ------------------------------------------------------------------------- */
+
+/*
+ * Rows of bf16 heads: element (l, t, h, c) at data + l * stride_layer +
+ * t * stride_token + h * stride_head + c (strides in elements, head_dim
+ * contiguous).  data 16-byte aligned, strides multiples of 8 and not negative.
+ * A view of one layer of an aircache_full_t with B * N rows of a token-major
+ * cache, of the parts of a fused projection, of packed sequences.
+ */
+typedef struct {
+    void *data;
+    int64_t stride_layer, stride_token, stride_head;
+} aircache_tokens_t;
+
+/* What aircache_rotate does to a head. */
+typedef struct {
+    int32_t n_layers;    /* L >= 1: layers in one call (weights and rows differ by layer, positions do not) */
+    int32_t n_tokens;    /* T >= 0 tokens per layer                                                       */
+    int32_t n_q_heads;   /* Hq >= 0                                                                       */
+    int32_t n_kv_heads;  /* Hkv >= 0; Hq + 2 * Hkv >= 1                                                    */
+    int32_t head_dim;    /* d in {64, 128}                                                                */
+    int32_t rotary_dim;  /* the first R channels are rotated; a multiple of 16, 0 <= R <= d               */
+    int32_t interleaved; /* 0: channel i turns with i + R/2; 1: channel 2i with 2i + 1                    */
+    int32_t n_axes;      /* rows of `positions`, 1 to 3                                                   */
+    int32_t sections[3]; /* how many of the R/2 frequencies follow each axis, in order; their sum is R/2  */
+    float eps;           /* of the norm, >= 0                                                             */
+    float factor;        /* times cos and sin (scalings for long contexts; 1 without); finite             */
+} aircache_rotary_t;
+
+/*
+ * Norms of queries and keys for each head, rotary positions, and the store of
+ * keys and values into the cache, in one pass.  For a head x of a query or key:
+ *   y = x * rsqrt(mean(x^2) + eps) * weight      (y = x where the weight is NULL)
+ *   (y_a, y_b) -> factor * (y_a cos - y_b sin, y_b cos + y_a sin) for the pair of frequency i, angle
+ *                 positions[axis(i)][t] * inv_freq[i]
+ * in fp32 (the angle is reduced in fp64: any 32-bit position), rounded to bf16
+ * once.  Values are copied.
+ *   q, k, v       inputs [L, T, Hq | Hkv, d].  q may be NULL with Hq = 0; k and v with Hkv = 0; v alone: no
+ *                 values are stored
+ *   positions     i32 [n_axes, T]
+ *   inv_freq      f32 [R/2]; positions and inv_freq may be NULL with R = 0
+ *   q_weight, k_weight  bf16 [L, d], 16-byte aligned, or NULL
+ *   q_out         [L, T, Hq, d]; may be q itself (same pointer and strides)
+ *   k_out, v_out  the cache's rows [L, n_rows, Hkv, d]; must not overlap the inputs
+ *   rows          i64 [T]: token t goes to row rows[t] of k_out and v_out; a row outside [0, n_rows) (padding,
+ *                 say -1) is not stored.  NULL: row t
+ * Rows that no token names stay as they are; tokens that name the same row
+ * leave one of them there.
+ */
+int aircache_rotate(const aircache_rotary_t *spec, const aircache_tokens_t *q, const aircache_tokens_t *k,
+                    const aircache_tokens_t *v, const int32_t *positions, const float *inv_freq,
+                    const void *q_weight, const void *k_weight, const aircache_tokens_t *q_out,
+                    const aircache_tokens_t *k_out, const aircache_tokens_t *v_out, const int64_t *rows,
+                    int64_t n_rows, void *cuda_stream);
+
+/* ---------------------------------------------------------------------------
+ * Behind the compression: the ragged cache in 8 bits.  (The paper keeps 16.)
+ * ------------------------------------------------------------------------- */
+
+/* Rows of a region that share a scale. */
+#define AIRCACHE_SCALE_ROWS 64
+
+/*
+ * The ragged cache of the same offsets and lens in 8 bits: k and v are e4m3
+ * [total_rows, Hkv, d] (one head a row in per-KV-head mode).  The rows
+ * 64j .. 64j+63 of region r (counted from offsets[r]) and one KV head share a
+ * scale, a power of two, at [offsets[r] / 64 + first_region + r + j, head] of
+ * k_scale and v_scale, f32 [scale_blocks, Hkv]: no two regions share a
+ * block, wherever they begin.  An element stands for code * scale.
+ * k and v 16-byte aligned.
+ */
+typedef struct {
+    void *k, *v;
+    float *k_scale, *v_scale;
+    int64_t *offsets;      /* [L*B + 1] rows, as aircache_budget wrote them */
+    int32_t *lens;         /* [L*B]     rows in use                         */
+    int64_t total_rows;    /* capacity of k and v in rows                   */
+    int64_t scale_blocks;  /* capacity of k_scale and v_scale in blocks, >= aircache_scale_blocks() */
+    int64_t first_region;  /* regions of the caches in front that share the buffers; 0 for a cache of its own */
+} aircache_quantized_t;
+
+/* Blocks of scales that a cache of total_rows rows needs: total_rows / 64 + first_region + L * B (L * B * Hkv with
+ * per_kv_head).  Host arithmetic only; negative = error code. */
+int64_t aircache_scale_blocks(const aircache_shape_t *shape, int64_t total_rows, int64_t first_region);
+
+/*
+ * The compressed cache in 8 bits: the scale of a block is the smallest power of
+ * two s >= 2^-126 with max |x| <= 448 s over the finite x of its rows in use, and
+ * x is held as the e4m3 number nearest to x / s (ties to even).  Infinities
+ * become +-448 s, NaN stays NaN.  Slack rows, and the scales of blocks that hold
+ * none in use, stay as they are.  out->offsets and out->lens must be the arrays of
+ * `cache`.  A region whose rows leave either buffer is left out; lens[r] beyond
+ * offsets[r+1] - offsets[r] counts as that.
+ */
+int aircache_quantize(const aircache_shape_t *shape, const aircache_ragged_t *cache, aircache_quantized_t *out,
+                      void *cuda_stream);
+
+/*
+ * aircache_append for the cache of 8 bits: the new token's K and V (bf16
+ * [L, B, Hkv, d]) go into the first free slack row of every region and
+ * lens[r] grows by one.  In a block that holds rows already the scale becomes the
+ * larger of its own and the one the new row asks for; where it grows, the rows
+ * that the block holds are rounded to the new scale (exact but for numbers
+ * below 2^-6 of it).  `appended` as in aircache_append.  A region without a
+ * free row (offsets on the device) is left as it is.
+ */
+int aircache_append_quantized(const aircache_shape_t *shape, aircache_quantized_t *cache, const void *k_new,
+                              const void *v_new, int32_t appended, void *cuda_stream);
+
+/*
+ * aircache_decode_attn over the cache of 8 bits:  out_h = sum_j
+ * softmax_j(scale * <q_h, k_g[j]>) * v_g[j] with the elements' values, bf16
+ * queries, fp32 accumulation, fp32 output.  A region with lens[r] = 0 yields
+ * zeros, and so does one whose rows leave the buffers.  The weights enter the second product as an fp16 head
+ * and an fp16 remainder (2^-22), below 2^-36 of the largest weight times the
+ * largest scale seen they vanish.  No wait in the kernel depends on another
+ * block.
+ */
+int aircache_decode_attn_quantized(const aircache_shape_t *shape, const aircache_quantized_t *cache, const void *q,
+                                   float *out, void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
 /*
  * Zeroes the head of a workspace (enqueued on the stream): the status word, the
  * tickets and the plans that decode launches keep from one call to the next

@@ -52,6 +52,23 @@ class Ragged(C.Structure):
                 ("total_rows", C.c_int64), ("first_row", C.c_int64)]
 
 
+class Tokens(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_layer", C.c_int64), ("stride_token", C.c_int64),
+                ("stride_head", C.c_int64)]
+
+
+class Rotary(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_tokens", "n_q_heads", "n_kv_heads", "head_dim", "rotary_dim",
+                                           "interleaved", "n_axes")] + [("sections", C.c_int32 * 3),
+                                                                        ("eps", C.c_float), ("factor", C.c_float)]
+
+
+class Quantized(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("offsets", C.c_void_p), ("lens", C.c_void_p), ("total_rows", C.c_int64),
+                ("scale_blocks", C.c_int64), ("first_region", C.c_int64)]
+
+
 _lib = None
 
 _SIGNATURES = {
@@ -77,6 +94,15 @@ _SIGNATURES = {
                                               C.c_void_p]),
     "aircache_append": (C.c_int, [C.POINTER(Shape), C.POINTER(Ragged), C.c_void_p, C.c_void_p, C.c_int32,
                                   C.c_void_p]),
+    "aircache_rotate": (C.c_int, [C.POINTER(Rotary), C.POINTER(Tokens), C.POINTER(Tokens), C.POINTER(Tokens), C.c_void_p,
+                                  C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(Tokens), C.POINTER(Tokens),
+                                  C.POINTER(Tokens), C.c_void_p, C.c_int64, C.c_void_p]),
+    "aircache_scale_blocks": (C.c_int64, [C.POINTER(Shape), C.c_int64, C.c_int64]),
+    "aircache_quantize": (C.c_int, [C.POINTER(Shape), C.POINTER(Ragged), C.POINTER(Quantized), C.c_void_p]),
+    "aircache_append_quantized": (C.c_int, [C.POINTER(Shape), C.POINTER(Quantized), C.c_void_p, C.c_void_p, C.c_int32,
+                                            C.c_void_p]),
+    "aircache_decode_attn_quantized": (C.c_int, [C.POINTER(Shape), C.POINTER(Quantized), C.c_void_p, C.c_void_p,
+                                                 C.c_void_p, C.c_int64, C.c_void_p]),
     "aircache_reset_status": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p]),
     "aircache_check_status": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p]),
     "aircache_selftest_wait_timeout": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p]),
@@ -186,6 +212,32 @@ def ragged_view(k, v, offsets, lens, total_rows: int, first_row: int = 0) -> Rag
     return Ragged(_ptr(k), _ptr(v), _ptr(offsets), _ptr(lens), total_rows, first_row)
 
 
+def tokens_view(t: torch.Tensor | None) -> Tokens | None:
+    """View of a bf16 tensor [T, H, d] or [L, T, H, d] (any strides, d contiguous); None stays None."""
+    if t is None:
+        return None
+    assert t.dtype == torch.bfloat16 and t.dim() in (3, 4) and (t.stride(-1) == 1 or t.shape[-1] == 1)
+    return Tokens(t.data_ptr(), t.stride(0) if t.dim() == 4 else 0, t.stride(-3), t.stride(-2))
+
+
+def rotary(n_layers, n_tokens, n_q_heads, n_kv_heads, head_dim, rotary_dim=None, interleaved=0, sections=None, eps=1e-6,
+           factor=1.0) -> Rotary:
+    """`sections`: frequencies per position axis, one entry an axis (default: one axis)."""
+    rotary_dim = head_dim if rotary_dim is None else rotary_dim
+    sections = [rotary_dim // 2] if sections is None else list(sections)
+    return Rotary(n_layers, n_tokens, n_q_heads, n_kv_heads, head_dim, rotary_dim, int(interleaved), len(sections),
+                  (C.c_int32 * 3)(*(sections + [0] * (3 - len(sections)))), eps, factor)
+
+
+def quantized_view(k, v, k_scale, v_scale, offsets, lens, total_rows: int, first_region: int = 0,
+                   scale_blocks: int | None = None) -> Quantized:
+    """`k`, `v`: one byte per element (e4m3 codes).  `scale_blocks` is k_scale's first size where that is a tensor."""
+    if scale_blocks is None:
+        scale_blocks = k_scale.shape[0]
+    return Quantized(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(offsets), _ptr(lens), total_rows,
+                     scale_blocks, first_region)
+
+
 # ------------------------------------------------------------------------------------------------
 # the C ABI, same names
 # ------------------------------------------------------------------------------------------------
@@ -293,6 +345,43 @@ def aircache_append(sh, cache, k_new, v_new, appended, stream=None, check=True) 
     return rc
 
 
+def aircache_rotate(spec, q, k, v, positions, inv_freq, q_weight, k_weight, q_out, k_out, v_out, rows, n_rows,
+                    stream=None, check=True) -> int:
+    rc = lib().aircache_rotate(C.byref(spec), _ref(q), _ref(k), _ref(v), _ptr(positions), _ptr(inv_freq),
+                               _ptr(q_weight), _ptr(k_weight), _ref(q_out), _ref(k_out), _ref(v_out), _ptr(rows),
+                               n_rows, _stream(stream))
+    if check:
+        _check("aircache_rotate", rc)
+    return rc
+
+
+def aircache_scale_blocks(sh: Shape, total_rows: int, first_region: int = 0) -> int:
+    return int(lib().aircache_scale_blocks(C.byref(sh), total_rows, first_region))
+
+
+def aircache_quantize(sh, cache, out, stream=None, check=True) -> int:
+    rc = lib().aircache_quantize(C.byref(sh), C.byref(cache), C.byref(out), _stream(stream))
+    if check:
+        _check("aircache_quantize", rc)
+    return rc
+
+
+def aircache_append_quantized(sh, cache, k_new, v_new, appended, stream=None, check=True) -> int:
+    rc = lib().aircache_append_quantized(C.byref(sh), C.byref(cache), _ptr(k_new), _ptr(v_new), appended,
+                                         _stream(stream))
+    if check:
+        _check("aircache_append_quantized", rc)
+    return rc
+
+
+def aircache_decode_attn_quantized(sh, cache, q, out, workspace, stream=None, check=True) -> int:
+    rc = lib().aircache_decode_attn_quantized(C.byref(sh), C.byref(cache), _ptr(q), _ptr(out), _ptr(workspace),
+                                              _nbytes(workspace), _stream(stream))
+    if check:
+        _check("aircache_decode_attn_quantized", rc)
+    return rc
+
+
 def aircache_reset_status(workspace, stream=None, check=True) -> int:
     rc = lib().aircache_reset_status(_ptr(workspace), _nbytes(workspace), _stream(stream))
     if check:
@@ -330,6 +419,10 @@ def aircache_pipeline_host(sh, h_full, full_elems, d_full_k, d_full_v, h_q_windo
     if check:
         _check("aircache_pipeline_host", rc)
     return rc
+
+
+def _ref(struct):
+    return None if struct is None else C.byref(struct)
 
 
 def _nbytes(t) -> int:

@@ -137,6 +137,48 @@ static int check_ragged(const aircache_shape_t *s, const aircache_ragged_t *c, b
     return AIRCACHE_OK;
 }
 
+static int check_quantized(const aircache_shape_t *s, const aircache_quantized_t *c) {
+    if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale || !c->offsets || !c->lens) return AIRCACHE_ERR_INVALID_ARG;
+    if (((uintptr_t)c->k & 15) || ((uintptr_t)c->v & 15) || ((uintptr_t)c->k_scale & 3) || ((uintptr_t)c->v_scale & 3) ||
+        ((uintptr_t)c->offsets & 7) || ((uintptr_t)c->lens & 3))
+        return AIRCACHE_ERR_ALIGNMENT;
+    if (c->first_region < 0) return AIRCACHE_ERR_INVALID_ARG;
+    if (c->total_rows < 1 || c->total_rows >= ((int64_t)1 << 31) || c->first_region >= ((int64_t)1 << 31))
+        return AIRCACHE_ERR_CAPACITY;
+    if (c->scale_blocks < c->total_rows / AIRCACHE_SCALE_ROWS + c->first_region + n_cells(s)) return AIRCACHE_ERR_CAPACITY;
+    return AIRCACHE_OK;
+}
+
+// Rows of heads for a kernel that moves 16 bytes at a time.
+static int check_tokens(const aircache_tokens_t *t) {
+    if (!t || !t->data) return AIRCACHE_ERR_INVALID_ARG;
+    if ((uintptr_t)t->data & 15) return AIRCACHE_ERR_ALIGNMENT;
+    const int64_t st[3] = {t->stride_layer, t->stride_token, t->stride_head};
+    for (int i = 0; i < 3; ++i) {
+        if (st[i] < 0) return AIRCACHE_ERR_INVALID_ARG;
+        if (st[i] % 8 != 0) return AIRCACHE_ERR_ALIGNMENT;
+    }
+    return AIRCACHE_OK;
+}
+
+// The same for rows that are written: no two elements in one place.
+static int check_tokens_out(const aircache_tokens_t *t, int64_t layers, int64_t rows, int64_t heads, int d) {
+    const int rc = check_tokens(t);
+    if (rc) return rc;
+    struct Axis { int64_t n, stride; } a[3] = {{layers, t->stride_layer}, {rows, t->stride_token}, {heads, t->stride_head}};
+    int64_t span = d;   // axes from the smallest stride on: each has to step over what the ones before it span
+    for (int taken = 0; taken < 3; ++taken) {
+        int least = -1;
+        for (int i = 0; i < 3; ++i)
+            if (a[i].n > 1 && (least < 0 || a[i].stride < a[least].stride)) least = i;
+        if (least < 0) break;
+        if (a[least].stride < span) return AIRCACHE_ERR_INVALID_ARG;
+        span += a[least].stride * (a[least].n - 1);
+        a[least].n = 1;
+    }
+    return AIRCACHE_OK;
+}
+
 // ---------------------------------------------------------------------------------------------
 // aircache_selftest_wait_timeout: the bounded wait on a barrier that nobody completes
 // ---------------------------------------------------------------------------------------------
@@ -312,6 +354,94 @@ int aircache_append(const aircache_shape_t *shape, aircache_ragged_t *cache, con
     if (((uintptr_t)k_new & 15) || ((uintptr_t)v_new & 15)) return AIRCACHE_ERR_ALIGNMENT;
     if (appended >= shape->slack) return AIRCACHE_ERR_CAPACITY;
     return launch_append(shape, cache, k_new, v_new, appended, (cudaStream_t)cuda_stream);
+}
+
+int aircache_rotate(const aircache_rotary_t *spec, const aircache_tokens_t *q, const aircache_tokens_t *k,
+                    const aircache_tokens_t *v, const int32_t *positions, const float *inv_freq,
+                    const void *q_weight, const void *k_weight, const aircache_tokens_t *q_out,
+                    const aircache_tokens_t *k_out, const aircache_tokens_t *v_out, const int64_t *rows,
+                    int64_t n_rows, void *cuda_stream) {
+    if (!spec) return AIRCACHE_ERR_INVALID_ARG;
+    const aircache_rotary_t &r = *spec;
+    if (r.n_layers < 1 || r.n_tokens < 0 || r.n_q_heads < 0 || r.n_kv_heads < 0 || n_rows < 0) return AIRCACHE_ERR_INVALID_ARG;
+    if (r.n_q_heads == 0 && r.n_kv_heads == 0) return AIRCACHE_ERR_INVALID_ARG;
+    if (r.n_q_heads > (1 << 20) || r.n_kv_heads > (1 << 20)) return AIRCACHE_ERR_UNSUPPORTED;
+    if (r.head_dim != 64 && r.head_dim != 128) return AIRCACHE_ERR_UNSUPPORTED;
+    if (r.rotary_dim < 0 || r.rotary_dim > r.head_dim) return AIRCACHE_ERR_INVALID_ARG;
+    if (r.rotary_dim % 16 != 0) return AIRCACHE_ERR_UNSUPPORTED;
+    if (r.interleaved != 0 && r.interleaved != 1) return AIRCACHE_ERR_INVALID_ARG;
+    if (!(r.eps >= 0.0f) || !isfinite(r.eps) || !isfinite(r.factor)) return AIRCACHE_ERR_INVALID_ARG;
+    if (r.rotary_dim > 0) {
+        if (r.n_axes < 1 || r.n_axes > 3 || !positions || !inv_freq) return AIRCACHE_ERR_INVALID_ARG;
+        int64_t sum = 0;
+        for (int i = 0; i < 3; ++i) {
+            if (r.sections[i] < 0 || (i >= r.n_axes && r.sections[i] != 0)) return AIRCACHE_ERR_INVALID_ARG;
+            sum += r.sections[i];
+        }
+        if (sum != r.rotary_dim / 2) return AIRCACHE_ERR_INVALID_ARG;
+    }
+    if (((uintptr_t)positions & 3) || ((uintptr_t)inv_freq & 3) || ((uintptr_t)q_weight & 15) ||
+        ((uintptr_t)k_weight & 15) || ((uintptr_t)rows & 7))
+        return AIRCACHE_ERR_ALIGNMENT;
+    int rc;
+    if (r.n_q_heads > 0) {
+        if ((rc = check_tokens(q))) return rc;
+        if ((rc = check_tokens_out(q_out, r.n_layers, r.n_tokens, r.n_q_heads, r.head_dim))) return rc;
+        if (q->data == q_out->data && (q->stride_layer != q_out->stride_layer || q->stride_token != q_out->stride_token ||
+                                       q->stride_head != q_out->stride_head))
+            return AIRCACHE_ERR_INVALID_ARG;
+    }
+    if (r.n_kv_heads > 0) {
+        if ((rc = check_tokens(k))) return rc;
+        if ((rc = check_tokens_out(k_out, r.n_layers, n_rows, r.n_kv_heads, r.head_dim))) return rc;
+        if (v) {
+            if ((rc = check_tokens(v))) return rc;
+            if ((rc = check_tokens_out(v_out, r.n_layers, n_rows, r.n_kv_heads, r.head_dim))) return rc;
+        }
+    }
+    if (r.n_tokens == 0) return AIRCACHE_OK;
+    return launch_rotate(spec, q, k, v, positions, inv_freq, q_weight, k_weight, q_out, k_out, v_out, rows, n_rows,
+                         (cudaStream_t)cuda_stream);
+}
+
+int64_t aircache_scale_blocks(const aircache_shape_t *shape, int64_t total_rows, int64_t first_region) {
+    const int rc = check_shape(shape);
+    if (rc) return rc;
+    if (total_rows < 0 || first_region < 0) return AIRCACHE_ERR_INVALID_ARG;
+    if (total_rows >= ((int64_t)1 << 31) || first_region >= ((int64_t)1 << 31)) return AIRCACHE_ERR_CAPACITY;
+    return total_rows / AIRCACHE_SCALE_ROWS + first_region + n_cells(shape);
+}
+
+int aircache_quantize(const aircache_shape_t *shape, const aircache_ragged_t *cache, aircache_quantized_t *out,
+                      void *cuda_stream) {
+    int rc = check_shape(shape);
+    if (rc) return rc;
+    if ((rc = check_ragged(shape, cache, true))) return rc;
+    if ((rc = check_quantized(shape, out))) return rc;
+    if (out->offsets != cache->offsets || out->lens != cache->lens) return AIRCACHE_ERR_INVALID_ARG;
+    return launch_quantize(shape, cache, out, (cudaStream_t)cuda_stream);
+}
+
+int aircache_append_quantized(const aircache_shape_t *shape, aircache_quantized_t *cache, const void *k_new,
+                              const void *v_new, int32_t appended, void *cuda_stream) {
+    int rc = check_shape(shape);
+    if (rc) return rc;
+    if ((rc = check_quantized(shape, cache))) return rc;
+    if (!k_new || !v_new || appended < 0) return AIRCACHE_ERR_INVALID_ARG;
+    if (((uintptr_t)k_new & 15) || ((uintptr_t)v_new & 15)) return AIRCACHE_ERR_ALIGNMENT;
+    if (appended >= shape->slack) return AIRCACHE_ERR_CAPACITY;
+    return launch_append_quantized(shape, cache, k_new, v_new, (cudaStream_t)cuda_stream);
+}
+
+int aircache_decode_attn_quantized(const aircache_shape_t *shape, const aircache_quantized_t *cache, const void *q,
+                                   float *out, void *workspace, int64_t workspace_bytes, void *cuda_stream) {
+    int rc = check_shape(shape);
+    if (rc) return rc;
+    if ((rc = check_quantized(shape, cache))) return rc;
+    if (!q || !out) return AIRCACHE_ERR_INVALID_ARG;
+    if (((uintptr_t)q & 15) || ((uintptr_t)out & 15)) return AIRCACHE_ERR_ALIGNMENT;
+    if ((rc = check_ws(shape, workspace, workspace_bytes))) return rc;
+    return launch_decode_quantized(shape, cache, q, out, workspace, (cudaStream_t)cuda_stream);
 }
 
 int aircache_reset_status(void *workspace, int64_t workspace_bytes, void *cuda_stream) {

@@ -168,6 +168,35 @@ int launch_decode_static(const aircache_shape_t *s, const aircache_ragged_t *c, 
 int launch_selftest_timeout(void *ws, cudaStream_t st);
 int launch_append(const aircache_shape_t *s, aircache_ragged_t *c, const void *k_new, const void *v_new,
                   int32_t appended, cudaStream_t st);
+int launch_rotate(const aircache_rotary_t *r, const aircache_tokens_t *q, const aircache_tokens_t *k,
+                  const aircache_tokens_t *v, const int32_t *positions, const float *inv_freq, const void *q_weight,
+                  const void *k_weight, const aircache_tokens_t *q_out, const aircache_tokens_t *k_out,
+                  const aircache_tokens_t *v_out, const int64_t *rows, int64_t n_rows, cudaStream_t st);
+int launch_quantize(const aircache_shape_t *s, const aircache_ragged_t *c, aircache_quantized_t *out, cudaStream_t st);
+int launch_append_quantized(const aircache_shape_t *s, aircache_quantized_t *c, const void *k_new, const void *v_new,
+                            cudaStream_t st);
+int launch_decode_quantized(const aircache_shape_t *s, const aircache_quantized_t *c, const void *q, float *out,
+                            void *ws, cudaStream_t st);
+
+#ifdef __CUDACC__
+// A launch that may start while the kernel before it on the stream ends (it waits with griddepcontrol.wait before it
+// touches memory).
+template <typename... Params, typename... Args>
+inline int launch_dependent(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    AIRCACHE_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, Params(args)...));
+    return AIRCACHE_OK;
+}
+#endif
 
 // ---------------------------------------------------------------------------------------------
 // device helpers

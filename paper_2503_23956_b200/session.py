@@ -6,9 +6,10 @@ from __future__ import annotations
 
 import torch
 
-from . import (Shape, aircache_budget, aircache_check_status, aircache_compact, aircache_decode_attn,
-               aircache_kept_per_sequence, aircache_reset_status, aircache_score, aircache_total_rows,
-               aircache_workspace_bytes, full_view, ragged_view)
+from . import (Shape, aircache_append_quantized, aircache_budget, aircache_check_status, aircache_compact,
+               aircache_decode_attn, aircache_decode_attn_quantized, aircache_kept_per_sequence, aircache_quantize,
+               aircache_reset_status, aircache_scale_blocks, aircache_score, aircache_total_rows,
+               aircache_workspace_bytes, full_view, quantized_view, ragged_view)
 
 
 class Session:
@@ -60,6 +61,25 @@ class Session:
 
     def decode(self, q, out=None, stream=None):
         aircache_decode_attn(self.sh, self.cache, q, self.out if out is None else out, self.ws, stream)
+
+    def quantize(self, stream=None):
+        """The compressed cache in 8 bits (self.k8, self.v8, self.k_scale, self.v_scale); its rows and lengths stay those
+        of the 16-bit one, whose k_c and v_c may then be dropped."""
+        if getattr(self, "cache8", None) is None:
+            blocks = aircache_scale_blocks(self.sh, self.rows)
+            self.k8 = torch.empty(self.k_c.shape, dtype=torch.uint8, device=self.dev)
+            self.v8 = torch.empty_like(self.k8)
+            self.k_scale = torch.empty((blocks, self.k_c.shape[1]), dtype=torch.float32, device=self.dev)
+            self.v_scale = torch.empty_like(self.k_scale)
+            self.cache8 = quantized_view(self.k8, self.v8, self.k_scale, self.v_scale, self.offsets, self.lens,
+                                         self.rows)
+        aircache_quantize(self.sh, self.cache, self.cache8, stream)
+
+    def append_quantized(self, k_new, v_new, appended, stream=None):
+        aircache_append_quantized(self.sh, self.cache8, k_new, v_new, appended, stream)
+
+    def decode_quantized(self, q, out=None, stream=None):
+        aircache_decode_attn_quantized(self.sh, self.cache8, q, self.out if out is None else out, self.ws, stream)
 
     def status(self) -> int:
         return aircache_check_status(self.ws, check=False)
