@@ -324,8 +324,8 @@ int aircache_append(const aircache_shape_t *shape, aircache_ragged_t *cache, con
                     const void *v_new, int32_t appended, void *cuda_stream);
 
 /* ---------------------------------------------------------------------------
- * In front of the compression: the prompt.  (The paper takes its keys and
- * values as given.)
+ * In front of the compression: the prompt.  (The paper takes keys, values and
+ * the prompt's attention as given.)
  * ------------------------------------------------------------------------- */
 
 /*
@@ -380,6 +380,47 @@ int aircache_rotate(const aircache_rotary_t *spec, const aircache_tokens_t *q, c
                     const void *q_weight, const void *k_weight, const aircache_tokens_t *q_out,
                     const aircache_tokens_t *k_out, const aircache_tokens_t *v_out, const int64_t *rows,
                     int64_t n_rows, void *cuda_stream);
+
+/* Packed sequences of one layer's prompt. */
+typedef struct {
+    int32_t n_seqs;      /* 0 <= S <= 1024                                                     */
+    int32_t q_tokens;    /* rows of q and out, >= 0                                            */
+    int32_t k_tokens;    /* rows of k and v, >= 0                                              */
+    int32_t n_q_heads;   /* Hq, a multiple of n_kv_heads with Hq / Hkv <= 16, Hq <= 1024        */
+    int32_t n_kv_heads;  /* Hkv >= 1                                                           */
+    int32_t head_dim;    /* d in {64, 128}                                                     */
+    int32_t causal;      /* 1: the last new token sees all keys, the one before all but one, ...
+                            0: every new token sees all keys of its sequence                   */
+    float scale;         /* normally 1 / sqrt(head_dim); > 0                                   */
+} aircache_prompt_t;
+
+/*
+ * Attention of one layer over whole prompts, packed one behind the other:
+ * sequence s owns rows q_offsets[s] .. q_offsets[s+1]-1 of q and out and rows
+ * k_offsets[s] .. k_offsets[s+1]-1 of k and v.  For its new token i (of n_q) and
+ * query head h, over the first n keys (of n_k; causal: n = n_k - n_q + i + 1),
+ *   out_h = sum_j softmax_j(scale * <q_h, k_g[j]>) * v_g[j]
+ * bf16 inputs, fp32 accumulation, weights rounded to bf16 for the second
+ * product, bf16 output.  A token that sees no key yields zeros.  n_k > n_q is a
+ * turn behind keys that are there already, n_q = 1 a single token.
+ *   q_offsets, k_offsets  i32 [S + 1], non-decreasing, within the rows given; k_offsets NULL: the same
+ *                 (offsets outside the buffers are clamped to them, nothing outside is read or written)
+ * Rows in front of the first and behind the last sequence stay as they are (NaN
+ * there and in other sequences reach nothing).  Within a sequence a value
+ * row that is not finite also reaches the tokens up to 255 before it, which it
+ * is masked for.  A key of minus infinity in a logit counts as masked.
+ */
+int aircache_prompt_attn(const aircache_prompt_t *spec, const aircache_tokens_t *q, const aircache_tokens_t *k,
+                         const aircache_tokens_t *v, const int32_t *q_offsets, const int32_t *k_offsets,
+                         const aircache_tokens_t *out, void *cuda_stream);
+
+/*
+ * Synchronises the stream and returns 0, or AIRCACHE_ERR_TIMEOUT if a bounded
+ * wait in aircache_prompt_attn gave up on the current device since the last call
+ * (a wait there is for the block's own copies and products; out is then
+ * incomplete).  Not to be called during a stream capture.
+ */
+int aircache_prompt_check_status(void *cuda_stream);
 
 /* ---------------------------------------------------------------------------
  * Behind the compression: the ragged cache in 8 bits.  (The paper keeps 16.)

@@ -63,6 +63,11 @@ class Rotary(C.Structure):
                                                                         ("eps", C.c_float), ("factor", C.c_float)]
 
 
+class Prompt(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_seqs", "q_tokens", "k_tokens", "n_q_heads", "n_kv_heads", "head_dim",
+                                           "causal")] + [("scale", C.c_float)]
+
+
 class Quantized(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
                 ("offsets", C.c_void_p), ("lens", C.c_void_p), ("total_rows", C.c_int64),
@@ -97,6 +102,9 @@ _SIGNATURES = {
     "aircache_rotate": (C.c_int, [C.POINTER(Rotary), C.POINTER(Tokens), C.POINTER(Tokens), C.POINTER(Tokens), C.c_void_p,
                                   C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(Tokens), C.POINTER(Tokens),
                                   C.POINTER(Tokens), C.c_void_p, C.c_int64, C.c_void_p]),
+    "aircache_prompt_attn": (C.c_int, [C.POINTER(Prompt), C.POINTER(Tokens), C.POINTER(Tokens), C.POINTER(Tokens),
+                                       C.c_void_p, C.c_void_p, C.POINTER(Tokens), C.c_void_p]),
+    "aircache_prompt_check_status": (C.c_int, [C.c_void_p]),
     "aircache_scale_blocks": (C.c_int64, [C.POINTER(Shape), C.c_int64, C.c_int64]),
     "aircache_quantize": (C.c_int, [C.POINTER(Shape), C.POINTER(Ragged), C.POINTER(Quantized), C.c_void_p]),
     "aircache_append_quantized": (C.c_int, [C.POINTER(Shape), C.POINTER(Quantized), C.c_void_p, C.c_void_p, C.c_int32,
@@ -229,6 +237,12 @@ def rotary(n_layers, n_tokens, n_q_heads, n_kv_heads, head_dim, rotary_dim=None,
                   (C.c_int32 * 3)(*(sections + [0] * (3 - len(sections)))), eps, factor)
 
 
+def prompt(n_seqs, q_tokens, k_tokens, n_q_heads, n_kv_heads, head_dim, scale=None, causal=1) -> Prompt:
+    if scale is None:
+        scale = 1.0 / math.sqrt(head_dim)
+    return Prompt(n_seqs, q_tokens, k_tokens, n_q_heads, n_kv_heads, head_dim, int(causal), scale)
+
+
 def quantized_view(k, v, k_scale, v_scale, offsets, lens, total_rows: int, first_region: int = 0,
                    scale_blocks: int | None = None) -> Quantized:
     """`k`, `v`: one byte per element (e4m3 codes).  `scale_blocks` is k_scale's first size where that is a tensor."""
@@ -352,6 +366,21 @@ def aircache_rotate(spec, q, k, v, positions, inv_freq, q_weight, k_weight, q_ou
                                n_rows, _stream(stream))
     if check:
         _check("aircache_rotate", rc)
+    return rc
+
+
+def aircache_prompt_attn(spec, q, k, v, q_offsets, k_offsets, out, stream=None, check=True) -> int:
+    rc = lib().aircache_prompt_attn(C.byref(spec), _ref(q), _ref(k), _ref(v), _ptr(q_offsets), _ptr(k_offsets),
+                                    _ref(out), _stream(stream))
+    if check:
+        _check("aircache_prompt_attn", rc)
+    return rc
+
+
+def aircache_prompt_check_status(stream=None, check=True) -> int:
+    rc = lib().aircache_prompt_check_status(_stream(stream))
+    if check:
+        _check("aircache_prompt_check_status", rc)
     return rc
 
 

@@ -13,7 +13,7 @@ LIB = os.path.join(PKG, "libaircache.so")
 BINDING_SOURCE = os.path.join(CSRC, "binding.c")
 BINDING = os.path.join(PKG, "_binding" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 SOURCES = ["api.cu", "score.cu", "score_cluster.cu", "score_dense.cu", "budget.cu", "compact.cu", "decode.cu", "rotate.cu",
-           "quantize.cu", "decode_quantized.cu"]
+           "quantize.cu", "decode_quantized.cu", "prompt.cu"]
 HEADERS = [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "ptx.cuh"), os.path.join(CSRC, "score.cuh"), os.path.join(CSRC, "quantize.cuh"),
            os.path.join(os.path.dirname(PKG), "include", "aircache.h")]
 

@@ -404,6 +404,28 @@ int aircache_rotate(const aircache_rotary_t *spec, const aircache_tokens_t *q, c
                          (cudaStream_t)cuda_stream);
 }
 
+int aircache_prompt_attn(const aircache_prompt_t *spec, const aircache_tokens_t *q, const aircache_tokens_t *k,
+                         const aircache_tokens_t *v, const int32_t *q_offsets, const int32_t *k_offsets,
+                         const aircache_tokens_t *out, void *cuda_stream) {
+    if (!spec) return AIRCACHE_ERR_INVALID_ARG;
+    const aircache_prompt_t &s = *spec;
+    if (s.n_seqs < 0 || s.q_tokens < 0 || s.k_tokens < 0 || s.n_q_heads < 1 || s.n_kv_heads < 1) return AIRCACHE_ERR_INVALID_ARG;
+    if (s.n_q_heads % s.n_kv_heads != 0) return AIRCACHE_ERR_INVALID_ARG;
+    if (!(s.scale > 0.0f) || !isfinite(s.scale) || (s.causal != 0 && s.causal != 1)) return AIRCACHE_ERR_INVALID_ARG;
+    if (s.head_dim != 64 && s.head_dim != 128) return AIRCACHE_ERR_UNSUPPORTED;
+    if (s.n_q_heads / s.n_kv_heads > kMaxGroup || s.n_q_heads > 1024 || s.n_seqs > kMaxPromptSeqs) return AIRCACHE_ERR_UNSUPPORTED;
+    if (s.n_seqs == 0 || s.q_tokens == 0) return AIRCACHE_OK;
+    int rc;
+    if ((rc = check_tokens(q))) return rc;
+    if (s.k_tokens > 0 && ((rc = check_tokens(k)) || (rc = check_tokens(v)))) return rc;
+    if ((rc = check_tokens_out(out, 1, s.q_tokens, s.n_q_heads, s.head_dim))) return rc;
+    if (!q_offsets || (!k_offsets && s.k_tokens != s.q_tokens)) return AIRCACHE_ERR_INVALID_ARG;
+    if (((uintptr_t)q_offsets & 3) || ((uintptr_t)k_offsets & 3)) return AIRCACHE_ERR_ALIGNMENT;
+    return launch_prompt(spec, q, k, v, q_offsets, k_offsets, out, (cudaStream_t)cuda_stream);
+}
+
+int aircache_prompt_check_status(void *cuda_stream) { return prompt_status((cudaStream_t)cuda_stream); }
+
 int64_t aircache_scale_blocks(const aircache_shape_t *shape, int64_t total_rows, int64_t first_region) {
     const int rc = check_shape(shape);
     if (rc) return rc;

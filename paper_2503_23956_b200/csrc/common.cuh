@@ -16,6 +16,7 @@ constexpr int kMaxGroup = 16;         // query heads per KV head
 constexpr int kMaxRegions = 1792;     // L * B (the decode kernel keeps the unit prefix of all regions in shared memory)
 constexpr int kMaxDecodeCtas = 256;   // upper bound on the persistent decode grid (sizes the partial slots)
 constexpr int kMaxDevices = 64;       // devices whose properties are kept after the first look
+constexpr int kMaxPromptSeqs = 1024;  // packed sequences of a prompt attention call (every block looks through them)
 constexpr int kScoreKeyTile = 128;    // visual keys per CTA of the importance pass
 constexpr float kLog2e = 1.4426950408889634f;
 // status word left by aircache_compact when the device-side budgets / offsets / lists do not fit the buffers
@@ -172,6 +173,10 @@ int launch_rotate(const aircache_rotary_t *r, const aircache_tokens_t *q, const 
                   const aircache_tokens_t *v, const int32_t *positions, const float *inv_freq, const void *q_weight,
                   const void *k_weight, const aircache_tokens_t *q_out, const aircache_tokens_t *k_out,
                   const aircache_tokens_t *v_out, const int64_t *rows, int64_t n_rows, cudaStream_t st);
+int launch_prompt(const aircache_prompt_t *s, const aircache_tokens_t *q, const aircache_tokens_t *k,
+                  const aircache_tokens_t *v, const int32_t *q_offsets, const int32_t *k_offsets,
+                  const aircache_tokens_t *out, cudaStream_t st);
+int prompt_status(cudaStream_t st);
 int launch_quantize(const aircache_shape_t *s, const aircache_ragged_t *c, aircache_quantized_t *out, cudaStream_t st);
 int launch_append_quantized(const aircache_shape_t *s, aircache_quantized_t *c, const void *k_new, const void *v_new,
                             cudaStream_t st);

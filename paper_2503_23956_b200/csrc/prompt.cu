@@ -1,0 +1,437 @@
+// aircache_prompt_attn: causal attention of one layer over packed prompts, on the fifth-generation tensor cores.
+//
+//   out_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp2(scale log2(e) <q_i, k_j> - ref_i)
+//
+// Bound by the tensor core (4 d flop per query head, query and visible key) and, next to it, by the exponentials: an SM
+// multiplies a 128 x 128 x 128 tile in some 512 cycles and takes 16384 exponentials, one per logit, in 1024.
+//
+// Work.  The G query heads of a KV group read the same keys, so rows of a tile are (token, head of the group) pairs, the
+// head inside: 128 / G tokens (rounded down) of all G heads, 126 rows at G = 7.  A tile then spans few tokens, which keeps the part
+// that the causal mask throws away small, and a turn of a few tokens still fills rows.  A block takes two such tiles, one behind
+// the other, of one sequence and KV head, and goes over the keys in tiles of 128, all of them once.  Blocks are numbered from the
+// last tokens of the last sequence on: those with the most keys start first.
+//
+// Roles.  Warp 8: TMA producer, Q once, then K and V tiles through one ring.  Warp 9: one thread issues the MMAs: S_i = Q_i K^T
+// (M = 128 rows, N = 128 keys, both operands from shared memory, K-major) and O_i += P_i V (P_i from tensor memory, V with
+// the keys as the outer axis).  Warps 0-3 and 4-7: the softmax of tile 0 and 1, a thread a row, no exchange between
+// threads: S_i from tensor memory, exponentials, P_i in bf16 back over the columns of S_i.  While one tile's softmax runs, the
+// tensor core has the other tile's products.  MMAs of one thread are executed in order, so S_i of the next key tile is issued right behind
+// the product that reads P_i.
+//
+// The reference of a row moves only when a logit is more than 2^8 above it; then its warp rescales O_i in tensor
+// memory, behind the last product's commit.  Sums and O_i in fp32.  P is rounded to bf16 (2^-9 of a weight, averaged over
+// the keys, beside 2^-9 of the rounding of the output).
+//
+// The last key tile of a sequence may hold rows of the next one or of nothing: their logits are masked, and the V rows are
+// zeroed in shared memory before they are multiplied (0 * NaN).
+#include <cuda.h>
+
+#include <atomic>
+
+#include "common.cuh"
+#include "ptx.cuh"
+
+namespace aircache {
+
+namespace {
+
+__device__ uint32_t g_prompt_status;   // set when a bounded wait gave up
+
+constexpr int kKeys = 128;             // keys of a tile
+
+struct PromptParams {
+    const int32_t *q_offsets, *k_offsets;
+    char *out;
+    int64_t out_token, out_head;   // bytes
+    int n_seqs, q_tokens, k_tokens, n_kv_heads, G, tokens_per_tile, units, causal;
+    float sl2;
+};
+
+template <int D>
+struct PromptCfg {
+    static constexpr int HALVES = D / 64;
+    static constexpr int TILE = kKeys * D * 2;           // bytes of a Q, K or V tile
+    static constexpr int HALF = kKeys * 128;             // of 64 channels of it
+    static constexpr int SLOTS = D == 128 ? 5 : 8;
+    static constexpr int SMEM = 1024 + (2 + SLOTS) * TILE;
+    static constexpr int THREADS = 320;
+};
+
+// PV: bf16 x bf16 -> fp32, A from tensor memory (K-major), B from shared memory with N contiguous
+__device__ __forceinline__ void umma_bf16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
+        ::"r"(tmem_d), "r"(tmem_a), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// 128-byte swizzled tile whose rows are the K axis (keys) and whose 128 bytes are 64 elements of N: groups of 8 rows are
+// 1024 bytes apart, the next 64 elements of N kKeys rows.
+__device__ __forceinline__ uint64_t umma_desc_rows_are_k(uint32_t smem_addr) {
+    uint64_t d = umma_desc_sw128(smem_addr) & ~((uint64_t)0x3fff << 16);
+    return d | (uint64_t)((kKeys * 128) >> 4) << 16;
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
+          "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
+          "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+template <int D>
+__global__ void __launch_bounds__(PromptCfg<D>::THREADS, 1)
+prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+              const __grid_constant__ CUtensorMap tm_v, const PromptParams p) {
+    using C = PromptCfg<D>;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ uint64_t s_bars[1 + 2 * C::SLOTS + 6];
+    __shared__ uint32_t s_tmem;
+    __shared__ volatile int s_abort;
+    __shared__ int s_unit[5];   // sequence's q0, n_q, k0, n_k, first token
+    const uint32_t smem = (smem_u32(smem_raw) + 1023) & ~1023u;
+    const uint32_t q_smem = smem, ring = smem + 2 * C::TILE;
+    const uint32_t bars = smem_u32(s_bars);
+    const uint32_t q_full = bars, kv_full = bars + 8, kv_empty = kv_full + 8 * C::SLOTS, s_full = kv_empty + 8 * C::SLOTS,
+                   p_full = s_full + 16, o_done = p_full + 16;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int group = blockIdx.x % p.n_kv_heads, TPT = p.tokens_per_tile;
+    uint32_t *status = &g_prompt_status;
+
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (warp == 9) tmem_alloc(smem_u32(&s_tmem), 512);
+    if (warp == 8 && lane == 0) {
+        mbar_init(q_full, 1);
+        for (int i = 0; i < C::SLOTS; ++i) {
+            mbar_init(kv_full + 8 * i, 1);
+            mbar_init(kv_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(s_full + 8 * i, 1);
+            mbar_init(p_full + 8 * i, 128);
+            mbar_init(o_done + 8 * i, 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        s_abort = 0;
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (warp == 0) {   // the block's unit: counted from the last one back
+        int unit = p.units - 1 - (int)(blockIdx.x / p.n_kv_heads);
+        if (lane < 5) s_unit[lane] = 0;   // (a block of a grid larger than the units: no tokens)
+        __syncwarp();
+        int before = 0;
+        for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
+            const int s = s0 + lane;
+            int q0 = 0, n_q = 0, n = 0;
+            if (s < p.n_seqs) {
+                q0 = min(max(p.q_offsets[s], 0), p.q_tokens);
+                n_q = min(max(p.q_offsets[s + 1], q0), p.q_tokens) - q0;
+                n = (n_q + 2 * TPT - 1) / (2 * TPT);
+            }
+            int incl = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int x = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += x;
+            }
+            const int mine = before + incl - n;
+            if (unit >= mine && unit < mine + n) {
+                const int k0 = min(max(p.k_offsets[s], 0), p.k_tokens);
+                s_unit[0] = q0;
+                s_unit[1] = n_q;
+                s_unit[2] = k0;
+                s_unit[3] = min(max(p.k_offsets[s + 1], k0), p.k_tokens) - k0;
+                s_unit[4] = (unit - mine) * 2 * TPT;
+            }
+            before += __shfl_sync(0xffffffffu, incl, 31);
+            if (before > unit) break;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    const int q0 = s_unit[0], n_q = s_unit[1], k0 = s_unit[2], n_k = s_unit[3], first = s_unit[4];
+    int tiles[2];   // key tiles of each row tile
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int t0 = first + i * TPT, last = min(t0 + TPT, n_q) - 1;
+        const int seen = t0 >= n_q ? 0 : min(n_k, p.causal ? n_k - n_q + last + 1 : n_k);
+        tiles[i] = seen <= 0 ? 0 : (seen + kKeys - 1) / kKeys;
+    }
+    const int n_tiles = max(tiles[0], tiles[1]);
+
+    if (warp == 8) {
+        if (lane == 0 && n_tiles > 0) {
+            const int rows = TPT * p.G;
+            const int n_row_tiles = tiles[1] > 0 ? 2 : 1;   // (the second has keys whenever it has tokens and the first has)
+            mbar_expect_tx(q_full, 2 * C::HALVES * 128 * rows);
+            for (int i = 0; i < 2; ++i)
+                for (int h = 0; h < C::HALVES; ++h)   // (the second tile again where there is none: the barrier counts both)
+                    tma_load_3d(q_smem + i * C::TILE + h * C::HALF, &tm_q, h * 64, group * p.G,
+                                q0 + first + (i < n_row_tiles ? i : 0) * TPT, q_full);
+            int slot = 0, phase = 0;
+            for (int c = 0; c < 2 * n_tiles; ++c) {
+                if (c >= C::SLOTS && !mbar_wait(kv_empty + 8 * slot, phase ^ 1, &s_abort, status, 1)) break;
+                mbar_expect_tx(kv_full + 8 * slot, C::TILE);
+                for (int h = 0; h < C::HALVES; ++h)
+                    tma_load_3d(ring + slot * C::TILE + h * C::HALF, c & 1 ? &tm_v : &tm_k, h * 64, group, k0 + (c >> 1) * kKeys,
+                                kv_full + 8 * slot);
+                if (++slot == C::SLOTS) { slot = 0; phase ^= 1; }
+            }
+        }
+    } else if (warp == 9) {
+        if (n_tiles > 0) {
+            const uint32_t idesc_s = umma_idesc_bf16(128, kKeys);
+            const uint32_t idesc_o = umma_idesc_bf16(128, D) | 1u << 16;   // B with N contiguous
+            bool ok = __all_sync(0xffffffffu, mbar_wait(q_full, 0, &s_abort, status, 2));
+            int seen = 0;   // tiles of the ring whose arrival has been waited for
+            auto arrived = [&](int c) {
+                for (; ok && seen <= c; ++seen)
+                    ok = __all_sync(0xffffffffu, mbar_wait(kv_full + 8 * (seen % C::SLOTS), seen / C::SLOTS & 1, &s_abort, status, 3));
+                tc_fence_after();
+            };
+            auto scores = [&](int i, int j) {   // S_i = Q_i K_j^T
+                if (elect_one()) {
+                    const uint32_t k_tile = ring + (2 * j % C::SLOTS) * C::TILE;
+#pragma unroll
+                    for (int s = 0; s < D / 16; ++s)
+                        umma_bf16(tmem + i * kKeys, umma_desc_sw128(q_smem + i * C::TILE + (s >> 2) * C::HALF + (s & 3) * 32),
+                                  umma_desc_sw128(k_tile + (s >> 2) * C::HALF + (s & 3) * 32), idesc_s, s > 0);
+                    umma_commit(s_full + 8 * i);
+                }
+                __syncwarp();
+            };
+            auto release = [&](int c) {
+                if (elect_one()) umma_commit(kv_empty + 8 * (c % C::SLOTS));
+                __syncwarp();
+            };
+            arrived(0);
+            for (int i = 0; i < 2; ++i)
+                if (ok && tiles[i] > 0) scores(i, 0);
+            if (ok) release(0);
+            for (int j = 0; ok && j < n_tiles; ++j) {
+                const uint32_t v_tile = ring + ((2 * j + 1) % C::SLOTS) * C::TILE;
+                arrived(2 * j + 1);
+                if (!ok) break;
+                const int rows = n_k - j * kKeys;
+                if (rows < kKeys) {   // keys behind the sequence's last: zeros
+                    for (int e = lane; e < (kKeys - rows) * C::HALVES * 8; e += 32) {
+                        const uint32_t at = v_tile + (e / ((kKeys - rows) * 8)) * C::HALF + rows * 128 + e % ((kKeys - rows) * 8) * 16;
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                }
+                for (int i = 0; i < 2 && ok; ++i) {
+                    if (j < tiles[i]) {
+                        ok = __all_sync(0xffffffffu, mbar_wait(p_full + 8 * i, j & 1, &s_abort, status, 4));
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int s = 0; s < kKeys / 16; ++s)
+                                umma_bf16_ts(tmem + 256 + i * 128, tmem + i * kKeys + s * 8, umma_desc_rows_are_k(v_tile + s * 2048),
+                                             idesc_o, j > 0 || s > 0);
+                            umma_commit(o_done + 8 * i);
+                        }
+                        __syncwarp();
+                    }
+                    if (i == 1) release(2 * j + 1);
+                    if (j + 1 < tiles[i]) {
+                        arrived(2 * j + 2);
+                        if (ok) scores(i, j + 1);
+                    }
+                }
+                if (ok && j + 1 < n_tiles) release(2 * j + 2);
+            }
+        }
+    } else {
+        const int i = warp >> 2, row = tid & 127, n = tiles[i];
+        const int token = first + i * TPT + row / p.G;
+        const bool used = row < TPT * p.G && token < n_q;
+        const int t0 = first + i * TPT;
+        const int limit = !used ? 0 : max(0, min(n_k, p.causal ? n_k - n_q + token + 1 : n_k));
+        const int all_see = p.causal ? n_k - n_q + t0 + 1 : n_k;   // keys that every token of the tile sees
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;          // 32 * (warp % 4) tensor-memory lanes
+        const uint32_t s_at = tmem + i * kKeys + lanes, o_at = tmem + 256 + i * 128 + lanes;
+        float ref = -1e30f;
+        float2 sum = make_float2(0.f, 0.f);
+        bool ok = true;
+        for (int j = 0; j < n; ++j) {
+            ok = mbar_wait(s_full + 8 * i, j & 1, &s_abort, status, 5);
+            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+            tc_fence_after();
+            uint32_t x[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld32_issue(s_at + c * 32, x[c]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld_wait(x[c]);
+            if ((j + 1) * kKeys > all_see || (j + 1) * kKeys > n_k) {
+                const int left = limit - j * kKeys;
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (c * 32 + e >= left) x[c][e] = 0xff800000u;
+            }
+            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int e = 0; e < 32; e += 2)
+                    top[c] = fmaxf(top[c], fmaxf(__uint_as_float(x[c][e]), __uint_as_float(x[c][e + 1])));
+            const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.sl2;
+            const bool moves = now > ref + 8.f;
+            if (__any_sync(0xffffffffu, moves)) {
+                const float to = moves ? now : ref, shrink = fast_exp2(ref - to);
+                ref = to;
+                sum.x *= shrink;
+                sum.y *= shrink;
+                if (j > 0) {   // O_i of the key tiles before: its last product has to be done
+                    ok = mbar_wait(o_done + 8 * i, (j - 1) & 1, &s_abort, status, 6);
+                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c = 0; c < D / 32; ++c) {
+                        uint32_t o[32];
+                        tmem_ld32_issue(o_at + c * 32, o);
+                        tmem_ld_wait(o);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
+                        tmem_st32(o_at + c * 32, o);
+                    }
+                }
+            }
+            const float2 scale2 = make_float2(p.sl2, p.sl2), ref2 = make_float2(-ref, -ref);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t w[32];
+#pragma unroll
+                for (int e = 0; e < 64; e += 2) {
+                    const float2 y = fma2(make_float2(__uint_as_float(x[2 * h + e / 32][e % 32]), __uint_as_float(x[2 * h + e / 32][e % 32 + 1])),
+                                          scale2, ref2);
+                    const float2 z = make_float2(fast_exp2(y.x), fast_exp2(y.y));
+                    sum = add2(sum, z);
+                    w[e / 2] = pack_bf16(z.x, z.y);
+                }
+                tmem_st32(s_at + h * 32, w);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            mbar_arrive(p_full + 8 * i);
+        }
+        float o_scale = 0.f;
+        if (ok && n > 0) {
+            ok = mbar_wait(o_done + 8 * i, (n - 1) & 1, &s_abort, status, 7);
+            ok = __all_sync(0xffffffffu, ok);
+            tc_fence_after();
+            const float l = sum.x + sum.y;
+            o_scale = l == 0.f ? 0.f : 1.f / l;
+        }
+        if (ok) {
+            char *to = p.out + (int64_t)(q0 + token) * p.out_token + (int64_t)(group * p.G + row % p.G) * p.out_head;
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t o[32];
+                if (n > 0) {
+                    tmem_ld32_issue(o_at + c * 32, o);
+                    tmem_ld_wait(o);
+                }
+                if (used) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int b = 0; b < 4; ++b)
+                            w[b] = n > 0 && limit > 0 ? pack_bf16(__uint_as_float(o[8 * e + 2 * b]) * o_scale, __uint_as_float(o[8 * e + 2 * b + 1]) * o_scale) : 0;
+                        *reinterpret_cast<uint4 *>(to + c * 64 + e * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+            }
+        }
+    }
+    // Every copy and product has been waited for by the roles above unless a wait gave up; then the ones in flight get
+    // their time (bounded) before the block's memory goes.
+    tc_fence_before();
+    __syncthreads();
+    if (s_abort && tid == 0)
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+    __syncthreads();
+    if (warp == 9) tmem_dealloc(tmem, 512);
+}
+
+// bf16 rows of heads as a 3-D tensor (d, heads, tokens); a box is 64 channels x `heads` x `tokens`.
+int tokens_map(CUtensorMap *tm, const aircache_tokens_t *t, int d, int heads, int64_t tokens, int box_heads, int box_tokens) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) { set_last_cuda_error(cudaErrorSymbolNotFound); return AIRCACHE_ERR_CUDA; }
+    const cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)tokens};
+    const cuuint64_t strides[2] = {(cuuint64_t)(heads > 1 ? t->stride_head * 2 : d * 2),
+                                   (cuuint64_t)(tokens > 1 ? t->stride_token * 2 : d * 2)};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_tokens}, estr[3] = {1, 1, 1};
+    const CUresult rc = fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, t->data, dims, strides, box, estr,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return rc == CUDA_SUCCESS ? AIRCACHE_OK : AIRCACHE_ERR_UNSUPPORTED;
+}
+
+template <int D>
+int launch_d(const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const PromptParams &p, int dev, cudaStream_t st) {
+    static std::atomic<uint64_t> allowed[kMaxDevices];
+    const int rc = allow_shared_memory((const void *)prompt_kernel<D>, PromptCfg<D>::SMEM, dev, allowed);
+    if (rc) return rc;
+    return launch_dependent(prompt_kernel<D>, dim3((unsigned)(p.units * p.n_kv_heads)), dim3(PromptCfg<D>::THREADS), PromptCfg<D>::SMEM, st,
+                            tm_q, tm_k, tm_v, p);
+}
+
+}  // namespace
+
+int launch_prompt(const aircache_prompt_t *s, const aircache_tokens_t *q, const aircache_tokens_t *k,
+                  const aircache_tokens_t *v, const int32_t *q_offsets, const int32_t *k_offsets,
+                  const aircache_tokens_t *out, cudaStream_t st) {
+    PromptParams p = {};
+    p.q_offsets = q_offsets;
+    p.k_offsets = k_offsets ? k_offsets : q_offsets;
+    p.out = static_cast<char *>(out->data);
+    p.out_token = 2 * out->stride_token;
+    p.out_head = 2 * out->stride_head;
+    p.n_seqs = s->n_seqs;
+    p.q_tokens = s->q_tokens;
+    p.k_tokens = s->k_tokens;
+    p.n_kv_heads = s->n_kv_heads;
+    p.G = s->n_q_heads / s->n_kv_heads;
+    p.tokens_per_tile = 128 / p.G;
+    p.causal = s->causal;
+    p.sl2 = s->scale * kLog2e;
+    const int64_t units = s->q_tokens / (2 * p.tokens_per_tile) + s->n_seqs;   // at least as many as there are
+    if (units * s->n_kv_heads >= ((int64_t)1 << 31)) return AIRCACHE_ERR_UNSUPPORTED;
+    p.units = (int)units;
+    int dev = 0, sms = 0, rc = current_device(&dev, &sms);
+    if (rc) return rc;
+    CUtensorMap tm_q, tm_k, tm_v;
+    if ((rc = tokens_map(&tm_q, q, s->head_dim, s->n_q_heads, s->q_tokens, p.G, p.tokens_per_tile))) return rc;
+    const bool keys = s->k_tokens > 0;   // (without keys nothing is loaded)
+    if ((rc = tokens_map(&tm_k, keys ? k : q, s->head_dim, keys ? s->n_kv_heads : 1, keys ? s->k_tokens : 1, 1, kKeys))) return rc;
+    if ((rc = tokens_map(&tm_v, keys ? v : q, s->head_dim, keys ? s->n_kv_heads : 1, keys ? s->k_tokens : 1, 1, kKeys))) return rc;
+    return s->head_dim == 64 ? launch_d<64>(tm_q, tm_k, tm_v, p, dev, st) : launch_d<128>(tm_q, tm_k, tm_v, p, dev, st);
+}
+
+int prompt_status(cudaStream_t st) {
+    uint32_t word = 0;
+    const uint32_t zero = 0;
+    AIRCACHE_CUDA_TRY(cudaMemcpyFromSymbolAsync(&word, g_prompt_status, sizeof word, 0, cudaMemcpyDeviceToHost, st));
+    AIRCACHE_CUDA_TRY(cudaStreamSynchronize(st));
+    if (!word) return AIRCACHE_OK;
+    AIRCACHE_CUDA_TRY(cudaMemcpyToSymbolAsync(g_prompt_status, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, st));
+    AIRCACHE_CUDA_TRY(cudaStreamSynchronize(st));
+    return AIRCACHE_ERR_TIMEOUT;
+}
+
+}  // namespace aircache
