@@ -142,7 +142,7 @@ def exported_symbols() -> list[str]:
     return list(_SIGNATURES)
 
 
-_native = None   # (module, addresses of aircache_decode_attn and aircache_decode_step) once CUDA is up; False: not to be had
+_native = None   # (module, addresses of the entry points that it calls) once CUDA is up; False: not to be had
 
 # torch's current device and the raw handle of its current stream: names that torch keeps to itself, hence looked up once
 # and done without where they are missing
@@ -164,10 +164,11 @@ def _per_token_calls():
         if _raw_device is None or _raw_stream is None:
             _native = False
             return _native
-        _binding.setup(Shape, Ragged, _raw_device, _raw_stream)
+        _binding.setup(Shape, Ragged, _raw_device, _raw_stream, Tokens, Rotary, Prompt, Quantized)
         handle = lib()
-        _native = (_binding, C.cast(handle.aircache_decode_attn, C.c_void_p).value,
-                   C.cast(handle.aircache_decode_step, C.c_void_p).value)
+        _native = (_binding,) + tuple(C.cast(getattr(handle, name), C.c_void_p).value for name in
+                                      ("aircache_decode_attn", "aircache_decode_step", "aircache_decode_attn_quantized",
+                                       "aircache_append_quantized", "aircache_rotate", "aircache_prompt_attn"))
     return _native
 
 
@@ -361,17 +362,36 @@ def aircache_append(sh, cache, k_new, v_new, appended, stream=None, check=True) 
 
 def aircache_rotate(spec, q, k, v, positions, inv_freq, q_weight, k_weight, q_out, k_out, v_out, rows, n_rows,
                     stream=None, check=True) -> int:
-    rc = lib().aircache_rotate(C.byref(spec), _ref(q), _ref(k), _ref(v), _ptr(positions), _ptr(inv_freq),
-                               _ptr(q_weight), _ptr(k_weight), _ref(q_out), _ref(k_out), _ref(v_out), _ptr(rows),
-                               n_rows, _stream(stream))
+    native = _native or _per_token_calls()
+    rc = None
+    if native:
+        try:
+            rc = native[0].rotate(native[5], spec, q, k, v, positions, inv_freq, q_weight, k_weight, q_out, k_out, v_out,
+                                  rows, n_rows, stream)
+        except TypeError:   # (before the call) perhaps an argument of a kind that only ctypes takes
+            if not isinstance(spec, Rotary):
+                raise
+    if rc is None:
+        rc = lib().aircache_rotate(C.byref(spec), _ref(q), _ref(k), _ref(v), _ptr(positions), _ptr(inv_freq),
+                                   _ptr(q_weight), _ptr(k_weight), _ref(q_out), _ref(k_out), _ref(v_out), _ptr(rows),
+                                   n_rows, _stream(stream))
     if check:
         _check("aircache_rotate", rc)
     return rc
 
 
 def aircache_prompt_attn(spec, q, k, v, q_offsets, k_offsets, out, stream=None, check=True) -> int:
-    rc = lib().aircache_prompt_attn(C.byref(spec), _ref(q), _ref(k), _ref(v), _ptr(q_offsets), _ptr(k_offsets),
-                                    _ref(out), _stream(stream))
+    native = _native or _per_token_calls()
+    rc = None
+    if native:
+        try:
+            rc = native[0].prompt_attn(native[6], spec, q, k, v, q_offsets, k_offsets, out, stream)
+        except TypeError:
+            if not isinstance(spec, Prompt):
+                raise
+    if rc is None:
+        rc = lib().aircache_prompt_attn(C.byref(spec), _ref(q), _ref(k), _ref(v), _ptr(q_offsets), _ptr(k_offsets),
+                                        _ref(out), _stream(stream))
     if check:
         _check("aircache_prompt_attn", rc)
     return rc
@@ -396,16 +416,34 @@ def aircache_quantize(sh, cache, out, stream=None, check=True) -> int:
 
 
 def aircache_append_quantized(sh, cache, k_new, v_new, appended, stream=None, check=True) -> int:
-    rc = lib().aircache_append_quantized(C.byref(sh), C.byref(cache), _ptr(k_new), _ptr(v_new), appended,
-                                         _stream(stream))
+    native = _native or _per_token_calls()
+    rc = None
+    if native:
+        try:
+            rc = native[0].append_quantized(native[4], sh, cache, k_new, v_new, appended, stream)
+        except TypeError:
+            if not (isinstance(sh, Shape) and isinstance(cache, Quantized)):
+                raise
+    if rc is None:
+        rc = lib().aircache_append_quantized(C.byref(sh), C.byref(cache), _ptr(k_new), _ptr(v_new), appended,
+                                             _stream(stream))
     if check:
         _check("aircache_append_quantized", rc)
     return rc
 
 
 def aircache_decode_attn_quantized(sh, cache, q, out, workspace, stream=None, check=True) -> int:
-    rc = lib().aircache_decode_attn_quantized(C.byref(sh), C.byref(cache), _ptr(q), _ptr(out), _ptr(workspace),
-                                              _nbytes(workspace), _stream(stream))
+    native = _native or _per_token_calls()
+    rc = None
+    if native:
+        try:
+            rc = native[0].decode_attn_quantized(native[3], sh, cache, q, out, workspace, stream)
+        except TypeError:
+            if not (isinstance(sh, Shape) and isinstance(cache, Quantized)):
+                raise
+    if rc is None:
+        rc = lib().aircache_decode_attn_quantized(C.byref(sh), C.byref(cache), _ptr(q), _ptr(out), _ptr(workspace),
+                                                  _nbytes(workspace), _stream(stream))
     if check:
         _check("aircache_decode_attn_quantized", rc)
     return rc

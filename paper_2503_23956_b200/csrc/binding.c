@@ -1,11 +1,13 @@
-/* The marshalling of the two entry points that a decoder calls for every token (aircache_decode_attn and
- * aircache_decode_step), natively: a kernel of theirs may take 5 us, and through ctypes the arguments alone took 2.4 and
- * 3.1 us of host time; here 0.6 and 0.8.  Same arguments, same function in libaircache.so, same return code. */
+/* The marshalling of the entry points that a decoder calls for every token (aircache_decode_attn and aircache_decode_step,
+ * aircache_rotate, and aircache_append_quantized and aircache_decode_attn_quantized over the cache of 8 bits; with them
+ * aircache_prompt_attn, for short prompts), natively: a kernel of theirs may take 2 to 5 us, and through ctypes the
+ * arguments alone took 2.4 and 3.1 us of host time for the first two; here 0.6 and 0.8.  Same arguments, same function in
+ * libaircache.so, same return code. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <stdint.h>
 
-static PyObject *s_shape, *s_ragged;             /* the binding's structure types */
+static PyObject *s_shape, *s_ragged, *s_tokens, *s_rotary, *s_prompt, *s_quantized;   /* the binding's structure types */
 static PyObject *s_get_device, *s_get_stream;    /* torch's current device and its current stream's raw handle */
 static PyObject *s_data_ptr, *s_numel, *s_element_size;
 
@@ -19,6 +21,11 @@ static int struct_address(PyObject *o, PyObject *type, int64_t *w) {
     *w = (int64_t)(intptr_t)view.buf;
     PyBuffer_Release(&view);   /* the caller's reference keeps the structure */
     return 0;
+}
+
+static int struct_or_null(PyObject *o, PyObject *type, int64_t *w) {
+    if (o == Py_None) { *w = 0; return 0; }
+    return struct_address(o, type, w);
 }
 
 static int as_int(PyObject *o, int64_t *w) {
@@ -110,13 +117,93 @@ static PyObject *decode_step(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     return PyLong_FromLong(rc);
 }
 
-/* setup(Shape, Ragged, get_device, get_raw_stream), once */
+/* decode_attn_quantized(function address, shape, cache, q, out, workspace, stream) */
+static PyObject *decode_attn_quantized(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    int64_t f, w[7];
+    if (n != 7) { PyErr_SetString(PyExc_TypeError, "decode_attn_quantized takes 7 arguments"); return NULL; }
+    if (as_int(a[0], &f) || struct_address(a[1], s_shape, &w[0]) || struct_address(a[2], s_quantized, &w[1]) ||
+        address(a[3], &w[2]) || address(a[4], &w[3]) || tail(a[5], a[6], &w[4]))
+        return NULL;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = ((int (*)(const void *, const void *, const void *, float *, void *, int64_t, void *))(intptr_t)f)(
+        (const void *)w[0], (const void *)w[1], (const void *)w[2], (float *)w[3], (void *)w[4], w[5], (void *)w[6]);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* append_quantized(function address, shape, cache, k_new, v_new, appended, stream) */
+static PyObject *append_quantized(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    int64_t f, w[6];
+    if (n != 7) { PyErr_SetString(PyExc_TypeError, "append_quantized takes 7 arguments"); return NULL; }
+    if (as_int(a[0], &f) || struct_address(a[1], s_shape, &w[0]) || struct_address(a[2], s_quantized, &w[1]) ||
+        address(a[3], &w[2]) || address(a[4], &w[3]) || as_int(a[5], &w[4]) || stream_handle(a[6], &w[5]))
+        return NULL;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = ((int (*)(const void *, void *, const void *, const void *, int32_t, void *))(intptr_t)f)(
+        (const void *)w[0], (void *)w[1], (const void *)w[2], (const void *)w[3], (int32_t)w[4], (void *)w[5]);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* rotate(function address, spec, q, k, v, positions, inv_freq, q_weight, k_weight, q_out, k_out, v_out, rows, n_rows, stream) */
+static PyObject *rotate(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    int64_t f, w[14];
+    if (n != 15) { PyErr_SetString(PyExc_TypeError, "rotate takes 15 arguments"); return NULL; }
+    if (as_int(a[0], &f) || struct_address(a[1], s_rotary, &w[0])) return NULL;
+    for (int i = 1; i < 4; ++i)
+        if (struct_or_null(a[1 + i], s_tokens, &w[i]) || struct_or_null(a[8 + i], s_tokens, &w[7 + i])) return NULL;
+    for (int i = 4; i < 8; ++i)
+        if (address(a[1 + i], &w[i])) return NULL;
+    if (address(a[12], &w[11]) || as_int(a[13], &w[12]) || stream_handle(a[14], &w[13])) return NULL;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = ((int (*)(const void *, const void *, const void *, const void *, const void *, const void *, const void *,
+                   const void *, const void *, const void *, const void *, const void *, int64_t, void *))(intptr_t)f)(
+        (const void *)w[0], (const void *)w[1], (const void *)w[2], (const void *)w[3], (const void *)w[4],
+        (const void *)w[5], (const void *)w[6], (const void *)w[7], (const void *)w[8], (const void *)w[9],
+        (const void *)w[10], (const void *)w[11], w[12], (void *)w[13]);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* prompt_attn(function address, spec, q, k, v, q_offsets, k_offsets, out, stream) */
+static PyObject *prompt_attn(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+    (void)self;
+    int64_t f, w[8];
+    if (n != 9) { PyErr_SetString(PyExc_TypeError, "prompt_attn takes 9 arguments"); return NULL; }
+    if (as_int(a[0], &f) || struct_address(a[1], s_prompt, &w[0]) || struct_or_null(a[2], s_tokens, &w[1]) ||
+        struct_or_null(a[3], s_tokens, &w[2]) || struct_or_null(a[4], s_tokens, &w[3]) || address(a[5], &w[4]) ||
+        address(a[6], &w[5]) || struct_or_null(a[7], s_tokens, &w[6]) || stream_handle(a[8], &w[7]))
+        return NULL;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = ((int (*)(const void *, const void *, const void *, const void *, const void *, const void *, const void *,
+                   void *))(intptr_t)f)((const void *)w[0], (const void *)w[1], (const void *)w[2], (const void *)w[3],
+                                        (const void *)w[4], (const void *)w[5], (const void *)w[6], (void *)w[7]);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* setup(Shape, Ragged, get_device, get_raw_stream[, Tokens, Rotary, Prompt, Quantized]), once; without the last four, only
+ * decode_attn and decode_step may be called */
 static PyObject *setup(PyObject *self, PyObject *args) {
     (void)self;
-    PyObject *shape, *ragged, *dev, *stream;
-    if (!PyArg_ParseTuple(args, "O!O!OO", &PyType_Type, &shape, &PyType_Type, &ragged, &dev, &stream)) return NULL;
-    Py_INCREF(shape); Py_INCREF(ragged); Py_INCREF(dev); Py_INCREF(stream);
-    s_shape = shape; s_ragged = ragged; s_get_device = dev; s_get_stream = stream;
+    PyObject *dev, *stream, *t[6] = {NULL, NULL, NULL, NULL, NULL, NULL};
+    if (!PyArg_ParseTuple(args, "O!O!OO|O!O!O!O!", &PyType_Type, &t[0], &PyType_Type, &t[1], &dev, &stream, &PyType_Type,
+                          &t[2], &PyType_Type, &t[3], &PyType_Type, &t[4], &PyType_Type, &t[5]))
+        return NULL;
+    Py_INCREF(dev); Py_INCREF(stream);
+    for (int i = 0; i < 6; ++i) {
+        if (!t[i]) t[i] = (PyObject *)&PyType_Type;   /* no structure is of this type: a TypeError */
+        Py_INCREF(t[i]);
+    }
+    s_get_device = dev; s_get_stream = stream;
+    s_shape = t[0]; s_ragged = t[1]; s_tokens = t[2]; s_rotary = t[3]; s_prompt = t[4]; s_quantized = t[5];
     Py_RETURN_NONE;
 }
 
@@ -124,6 +211,10 @@ static PyMethodDef s_methods[] = {
     {"setup", setup, METH_VARARGS, NULL},
     {"decode_attn", (PyCFunction)(void (*)(void))decode_attn, METH_FASTCALL, NULL},
     {"decode_step", (PyCFunction)(void (*)(void))decode_step, METH_FASTCALL, NULL},
+    {"decode_attn_quantized", (PyCFunction)(void (*)(void))decode_attn_quantized, METH_FASTCALL, NULL},
+    {"append_quantized", (PyCFunction)(void (*)(void))append_quantized, METH_FASTCALL, NULL},
+    {"rotate", (PyCFunction)(void (*)(void))rotate, METH_FASTCALL, NULL},
+    {"prompt_attn", (PyCFunction)(void (*)(void))prompt_attn, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef s_module = {PyModuleDef_HEAD_INIT, "_binding", NULL, -1, s_methods, NULL, NULL, NULL, NULL};
 

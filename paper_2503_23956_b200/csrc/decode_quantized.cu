@@ -7,22 +7,28 @@
 // every e4m3 number exactly.  As in decode.cu they are taken transposed, S^T = K Q^T and O^T = V^T P^T: 16 keys
 // (channels) are the rows and the query heads the 8 columns of a tile.
 //
-// Work.  A tile is 16 rows of a region (one KV head's worth of them per warp; a block of scales is four tiles).  The tiles
-// of all items (an item is a region; or a region and KV head, where these do not outnumber the SMs) form one list, CTA c takes an
-// equal contiguous share of it.  In a CTA, warp (head, sub) takes every SUBS-th tile of the share.  What a warp reads it reads for
-// itself: every lane copies the very bytes that it will need for its fragments into its own places of a ring in shared
-// memory (cp.async, 16 bytes), so there is no barrier and no bank conflict, and no ldmatrix that would need 16-bit elements:
-//   K fragments   lane (g, t) = (lane / 4, lane % 4) holds channels 16t..16t+15 (and 64+16t..) of keys g and g + 8.  Which
+// Work.  A tile is 32 rows of a region (one KV head's worth of them per warp; a block of scales is two tiles); an item is a
+// region, or a region and KV head where these do not outnumber the SMs.
+//   More items than SMs: the tiles of all items form one list, of which CTA c takes an equal contiguous share; a table of
+//   the items is built in shared memory.
+//   Else: an item is cut into pieces of equal size for as many CTAs, and stays whole where that costs less than the merge of
+//   pieces would.  Every warp plans this in registers.
+// In a CTA, warp (head, sub) takes every SUBS-th tile of the CTA's part, through a ring of its own in shared memory that
+// one of its lanes fills by TMA (boxes of 16 rows of one head, 128-byte swizzle, mbarriers): no warp waits for another.  The fragments
+// are read as 16 bytes per lane, since ldmatrix has no form for 8-bit elements of 16-bit products:
+//   K fragments   lane (g, t) = (lane / 4, lane % 4) holds channels 32t..32t+31 of keys g and g + 8.  Which
 //                 channels form a step of the product is free as long as q is laid out alike.
 //   V fragments   lane (g, t) holds channels 16g..16g+15 of keys 2t, 2t+1, 2t+8, 2t+9, the keys whose weights movmatrix
 //                 brings it; a byte permutation pairs two keys.
-// A ring slot is refilled when its tile is done; the ring runs on over the end of an item.  At the end of an item's part the SUBS states of
-// a head merge in a tree; an item that lies in one CTA is written, otherwise the CTA stores an unnormalised partial
+// A ring runs on over the end of an item.  There the SUBS states of a head merge through the ring stages just read;
+// an item that lies in one CTA is written, otherwise the CTA stores an unnormalised partial
 // and takes a ticket of the item, and the one that draws the last merges all of them in order.  Nobody waits.
 //
 // Numbers.  q is scaled by a power of two per head, so that its largest magnitude is 2^7 to 2^8 in fp16: what is 2^-32 of it is lost.
 // The reference of the softmax follows the largest logit lazily (it moves when one is more than 2^4 above), p <= 2^4.  p
 // times its block's V scale over the largest V scale seen, times 2^11, is split into an fp16 head and remainder (22 bits).  Sums in fp32.
+#include <cuda.h>
+
 #include <atomic>
 
 #include "common.cuh"
@@ -34,7 +40,6 @@ namespace aircache {
 namespace {
 
 struct DecodeQParams {
-    const char *k, *v;
     const float *k_scale, *v_scale;
     const int64_t *offsets;
     const int32_t *lens;
@@ -42,6 +47,7 @@ struct DecodeQParams {
     float *out;          // the same
     int32_t *tickets;    // [items], zero between calls
     float *partials;     // [2 * CTAs][slot]
+    uint32_t *status;
     int64_t rows, scale_blocks, first_region;
     int items, split;    // split: KV heads per region where an item is a (region, head), else 1
     int row_heads;       // KV heads of a row in memory
@@ -49,21 +55,9 @@ struct DecodeQParams {
     float sl2;           // scale * log2(e)
 };
 
-constexpr int kTile = 16;
+constexpr int kTile = 32;               // rows of a warp's tile: two blocks of 16, the rows of an MMA and of a TMA box
+constexpr int kBlocks = kTile / 16;
 constexpr float kLift = 2048.f;   // of the weights, above fp16's subnormal numbers
-
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool valid) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_async8(uint32_t dst, const void *src, bool valid) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(valid ? 8 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void *src) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 __device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                               uint32_t b0, uint32_t b1) {
@@ -88,23 +82,30 @@ __device__ __forceinline__ float2 f16x2_f32(uint32_t h) {
     return r;
 }
 
+// the warps of one KV head
+__device__ __forceinline__ void head_barrier(int head, int threads) {
+    asm volatile("bar.sync %0, %1;" ::"r"(head + 1), "r"(threads) : "memory");
+}
+
 template <int D, int HEADS, int NT>
 struct DecodeQCfg {
-    static constexpr int WARPS = NT == 2 ? 8 : 16;
+    static constexpr int WARPS = 8;
     static constexpr int SUBS = WARPS / HEADS;
     static constexpr int THREADS = WARPS * 32;
     static constexpr int CHUNKS = D / 64;                  // 64 channels of K: 16 per lane
     static constexpr int MT = D / 16;                      // channel tiles of O^T
-    static constexpr int STAGE = 2 * kTile * D;            // bytes of a warp's tile, K and V
-    static constexpr int STAGES = NT == 2 ? (D == 128 ? 4 : 8) : (D == 128 ? 2 : 4);
-    static constexpr int STATE = NT * (MT * 4 + 4);        // floats of a lane's state
-    static constexpr int MERGE = HEADS * (SUBS / 2) * STATE * 32 * 4;
+    static constexpr int HALF = kTile * D;                 // bytes of a warp's tile of K or V
+    static constexpr int STAGE = 2 * HALF;
+    static constexpr int STAGES = D == 128 ? 3 : 6;
     static constexpr int RING = WARPS * STAGES * STAGE;
-    static constexpr int SCALES = WARPS * STAGES * 8;
+    static constexpr int BARS = WARPS * STAGES * 8;
     static constexpr int TABLES = (3 * kMaxRegions + 1) * 4;
-    static constexpr int SMEM = RING + SCALES + MERGE + TABLES;
-    static_assert(SMEM <= 232448 - 1024, "shared memory of a block");
+    static constexpr int SMEM = 1024 + RING + BARS + TABLES;
+    static_assert(MT * 4 * 32 * 4 <= STAGE, "a stage takes the sums of 8 heads");
+    static_assert(SMEM <= 232448 - 2048, "shared memory of a block");
 };
+
+constexpr int kWholeTiles = 32;   // an item stays whole up to this many tiles (by warps) above the equal share
 
 // largest i with P[i] <= u (P non-decreasing, P[0] = 0, u < P[n])
 __device__ __forceinline__ int find_item(const int *P, int n, int u) {
@@ -117,39 +118,131 @@ __device__ __forceinline__ int find_item(const int *P, int n, int u) {
 }
 
 template <int D, int HEADS, int NT>
-__global__ void __launch_bounds__(DecodeQCfg<D, HEADS, NT>::THREADS, 1) decode_quantized_kernel(DecodeQParams p) {
+__global__ void __launch_bounds__(DecodeQCfg<D, HEADS, NT>::THREADS, 1)
+decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const DecodeQParams p) {
     using C = DecodeQCfg<D, HEADS, NT>;
-    extern __shared__ __align__(128) unsigned char smem[];
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *smem = smem_raw + (1024 - (smem_u32(smem_raw) & 1023)) % 1024;
     unsigned char *s_ring = smem;
-    float *s_scales = reinterpret_cast<float *>(smem + C::RING);
-    float *s_merge = reinterpret_cast<float *>(smem + C::RING + C::SCALES);
-    int *s_P = reinterpret_cast<int *>(smem + C::RING + C::SCALES + C::MERGE);   // [items + 1] first tile of an item
+    int *s_P = reinterpret_cast<int *>(smem + C::RING + C::BARS);   // [items + 1] first tile of an item
     int *s_off = s_P + kMaxRegions + 1, *s_len = s_off + kMaxRegions;
-    __shared__ int s_sum[C::WARPS];
+    __shared__ float4 s_state[C::WARPS * 4];   // references and sums of a warp's heads
+    __shared__ int s_sum[C::WARPS], s_free[C::WARPS];
     __shared__ int s_last;
+    __shared__ volatile int s_abort;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, t = lane & 3;
     const int head = warp % HEADS, sub = warp / HEADS;
+    const uint32_t bars = smem_u32(smem + C::RING) + warp * (C::STAGES * 8);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (lane == 0) {
+        for (int i = 0; i < C::STAGES; ++i) mbar_init(bars + 8 * i, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (tid == 0) {
+        s_abort = 0;
+        asm volatile("prefetch.tensormap [%0];\nprefetch.tensormap [%1];" ::"l"(&tm_k), "l"(&tm_v) : "memory");
+    }
+    {   // asked into L2 ahead of the wait (no value is used): lengths, first rows, this block's share of the queries
+        const int regions = p.items / p.split;
+        if (tid * 128 < regions * 4) prefetch_l2(reinterpret_cast<const char *>(p.lens) + tid * 128);
+        if (tid * 128 < regions * 8) prefetch_l2(reinterpret_cast<const char *>(p.offsets) + tid * 128);
+        const int64_t bytes = (int64_t)p.items * p.Hq * D * 2, at = ((int64_t)tid * gridDim.x + blockIdx.x) * 128;
+        if (at < bytes) prefetch_l2(reinterpret_cast<const char *>(p.q) + at);
+    }
+    __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    // first tile, first row and rows of every item
-    {
-        constexpr int PER = (kMaxRegions + C::THREADS - 1) / C::THREADS;
-        int n[PER], sum = 0;
+    // The CTA's tiles [t0, t1) and, of the item that they begin in: its number, first tile, end, first row, rows.
+    const int cta = blockIdx.x;
+    const bool pieces = p.items <= (int)gridDim.x;
+    int t0, t1, item, item_first, item_end, item_off, n, c_first = 0, c_last = 0, total = 0, ctas = gridDim.x;
+    if (pieces) {
+        constexpr int RPL = (kMaxDecodeCtas + 31) / 32;
+        const int regions = p.items / p.split, rpl = (regions + 31) / 32;
+        int len[RPL], off[RPL], un[RPL], sum = 0, most = 0;
+#pragma unroll
+        for (int j = 0; j < RPL; ++j) {
+            const int r = lane * rpl + j;
+            len[j] = off[j] = 0;
+            un[j] = -1;
+            if (j < rpl && r < regions) {
+                len[j] = rows_in_use(p.offsets, p.lens, r, p.rows, p.first_region, p.scale_blocks);
+                off[j] = (int)p.offsets[r];
+                un[j] = (len[j] + kTile - 1) / kTile;
+                sum += un[j];
+                most = max(most, un[j]);
+            }
+        }
+        sum = __reduce_add_sync(0xffffffffu, sum) * p.split;
+        most = __reduce_max_sync(0xffffffffu, most);
+        const int share = max((sum + ctas - 1) / ctas, 1);
+        int cap = max(most, 1);
+        if (most > share + kWholeTiles / HEADS) {   // the smallest of share, 9/8 of it, ... whose pieces find a CTA each
+            for (cap = share; cap < most; cap += (cap + 7) / 8) {
+                int need = 0;
+#pragma unroll
+                for (int j = 0; j < RPL; ++j) need += un[j] < 0 ? 0 : max((un[j] + cap - 1) / cap, 1);
+                if ((int)__reduce_add_sync(0xffffffffu, need) * p.split <= ctas) break;
+            }
+        }
+        int mine = 0;
+#pragma unroll
+        for (int j = 0; j < RPL; ++j) mine += un[j] < 0 ? 0 : max((un[j] + cap - 1) / cap, 1);
+        int run = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, run, o);
+            if (lane >= o) run += x;
+        }
+        run -= mine;
+        int found = -1, f_un = 0, f_len = 0, f_off = 0, f_first = 0, f_pieces = 0;
+#pragma unroll
+        for (int j = 0; j < RPL; ++j) {
+            if (un[j] < 0) continue;
+            const int pc = max((un[j] + cap - 1) / cap, 1);
+            if (cta >= run * p.split && cta < (run + pc) * p.split) {
+                found = lane * rpl + j;
+                f_un = un[j]; f_len = len[j]; f_off = off[j]; f_first = run * p.split; f_pieces = pc;
+            }
+            run += pc;
+        }
+        const unsigned who = __ballot_sync(0xffffffffu, found >= 0);
+        if (who == 0) return;
+        const int src = __ffs(who) - 1;
+        found = __shfl_sync(0xffffffffu, found, src);
+        item_end = __shfl_sync(0xffffffffu, f_un, src);
+        n = __shfl_sync(0xffffffffu, f_len, src);
+        item_off = __shfl_sync(0xffffffffu, f_off, src);
+        f_first = __shfl_sync(0xffffffffu, f_first, src);
+        f_pieces = __shfl_sync(0xffffffffu, f_pieces, src);
+        const int h = (cta - f_first) / f_pieces, piece = (cta - f_first) % f_pieces;
+        item = found * p.split + h;
+        c_first = f_first + h * f_pieces;
+        c_last = c_first + f_pieces - 1;
+        item_first = 0;
+        t0 = (int)((int64_t)item_end * piece / f_pieces);
+        t1 = (int)((int64_t)item_end * (piece + 1) / f_pieces);
+        if (item_end == 0) {
+            for (int e = tid; e < p.Hq * D; e += C::THREADS) p.out[(int64_t)item * p.Hq * D + e] = 0.f;
+            return;
+        }
+    } else {
+        // first tile, first row and rows of every item
+        constexpr int PER = (kMaxRegions + C::THREADS) / C::THREADS;   // of kMaxRegions + 1 entries
+        int u[PER], sum = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int item = tid * PER + i;
-            n[i] = 0;
-            if (item < p.items) {
-                const int r = item / p.split;
-                const int len = rows_in_use(p.offsets, p.lens, r, p.rows, p.first_region, p.scale_blocks);
-                s_off[item] = (int)p.offsets[r];
-                s_len[item] = len;
-                n[i] = (len + kTile - 1) / kTile;
+            const int at = tid * PER + i;
+            u[i] = 0;
+            if (at < p.items) {
+                const int len = rows_in_use(p.offsets, p.lens, at, p.rows, p.first_region, p.scale_blocks);
+                s_off[at] = (int)p.offsets[at];
+                s_len[at] = len;
+                u[i] = (len + kTile - 1) / kTile;
             }
-            sum += n[i];
+            sum += u[i];
         }
         int incl = sum;
 #pragma unroll
@@ -163,94 +256,112 @@ __global__ void __launch_bounds__(DecodeQCfg<D, HEADS, NT>::THREADS, 1) decode_q
         for (int w = 0; w < warp; ++w) before += s_sum[w];
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int item = tid * PER + i;
-            if (item <= p.items) s_P[item] = before;
-            before += n[i];
+            const int at = tid * PER + i;
+            if (at <= p.items) s_P[at] = before;
+            before += u[i];
         }
         __syncthreads();
+        total = s_P[p.items];
+        for (int i = cta; i < p.items; i += gridDim.x)
+            if (s_len[i] == 0)
+                for (int e = tid; e < p.Hq * D; e += C::THREADS) p.out[(int64_t)i * p.Hq * D + e] = 0.f;
+        ctas = min(ctas, total);   // each of them has a tile
+        if (cta >= ctas) return;
+        t0 = (int)((int64_t)total * cta / ctas);
+        t1 = (int)((int64_t)total * (cta + 1) / ctas);
+        item = find_item(s_P, p.items, t0);
+        item_first = s_P[item];
+        item_end = s_P[item + 1];
+        item_off = s_off[item];
+        n = s_len[item];
     }
-    const int total = s_P[p.items], cta = blockIdx.x;
-    for (int i = cta; i < p.items; i += gridDim.x)
-        if (s_len[i] == 0)
-            for (int e = tid; e < p.Hq * D; e += C::THREADS) p.out[(int64_t)i * p.Hq * D + e] = 0.f;
-    const int ctas = min((int)gridDim.x, total);   // each of them has a tile
-    if (cta >= ctas) return;
-    const int t0 = (int)((int64_t)total * cta / ctas), t1 = (int)((int64_t)total * (cta + 1) / ctas);
 
-    const uint32_t ring = smem_u32(s_ring) + warp * (C::STAGES * C::STAGE) + lane * 16;
-    const uint32_t scales = smem_u32(s_scales) + warp * (C::STAGES * 8);
-    const float *my_scales = s_scales + warp * (C::STAGES * 2);
-    const unsigned char *my_ring = s_ring + warp * (C::STAGES * C::STAGE) + lane * 16;
-    const int64_t pitch = (int64_t)p.row_heads * D;
-
-    // the warp's tiles: tau = sub mod SUBS in [t0, t1)
-    const int first_item = find_item(s_P, p.items, t0);
-    int ask = t0 + (sub - t0 % C::SUBS + C::SUBS) % C::SUBS, ask_item = first_item, ask_stage = 0;
-    auto issue = [&]() {   // the next tile into the next stage of the ring
+    // the warp's tiles: tau = sub mod SUBS in [t0, t1); the ring is filled STAGES - 1 tiles ahead
+    const uint32_t ring = smem_u32(s_ring) + warp * (C::STAGES * C::STAGE);
+    int tau = t0 + (sub - t0 % C::SUBS + C::SUBS) % C::SUBS, stage = 0;
+    uint32_t parity = 0;
+    int ask = tau, ask_stage = 0, ask_item = item, ask_first = item_first, ask_end = item_end, ask_off = item_off, ask_n = n;
+    int ask_region = pieces ? item / p.split : item;
+    const int ask_head = pieces && p.split > 1 ? item - ask_region * p.split : head;
+    // places of the scales of the tiles in the ring, the next one first.  (Places, not values: a move of a value that is being
+    // loaded waits for it.)  A tile's scales are loaded while the one before it is worked on.
+    int scale_at[C::STAGES];
+    const float *const k_scales = p.k_scale + p.first_region * p.row_heads, *const v_scales = p.v_scale + p.first_region * p.row_heads;
+    auto issue = [&](int &place) {
+        place = 0;
         if (ask < t1) {
-            while (ask >= s_P[ask_item + 1]) ++ask_item;
-            const int row0 = (ask - s_P[ask_item]) * kTile, n = s_len[ask_item];
-            const int64_t o = s_off[ask_item];
-            const int r = ask_item / p.split;
-            const int h = p.split > 1 ? ask_item - r * p.split : head;
-            const int64_t base = (o + row0) * pitch + h * D;
-            const uint32_t dst = ring + ask_stage * C::STAGE;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int key = g + 8 * i;
-                const bool valid = row0 + key < n;
-                const char *src = p.k + base + (valid ? key * pitch : 0) + t * 16;
-#pragma unroll
-                for (int c = 0; c < C::CHUNKS; ++c) cp_async16(dst + (i * C::CHUNKS + c) * 512, src + c * 64, valid);
+            if (ask >= ask_end) {   // (a list of items only: a piece ends with its item or before)
+                while (ask >= s_P[ask_item + 1]) ++ask_item;
+                ask_region = ask_item;
+                ask_first = s_P[ask_item];
+                ask_end = s_P[ask_item + 1];
+                ask_off = s_off[ask_item];
+                ask_n = s_len[ask_item];
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int key = 2 * t + (i & 1) + 8 * (i >> 1);
-                const bool valid = row0 + key < n;
-                const char *src = p.v + base + (valid ? key * pitch : 0) + g * (D / 8);
-                if (D == 128) cp_async16(dst + kTile * D + i * 512, src, valid);
-                else cp_async8(dst + kTile * D + i * 256 - lane * 8, src, valid);
+            const int row0 = (ask - ask_first) * kTile;
+            if (lane == 0) {   // (the item's last tile may need one block only)
+                const uint32_t bar = bars + 8 * ask_stage, dst = ring + ask_stage * C::STAGE;
+                const bool both = row0 + 16 < ask_n;
+                mbar_expect_tx(bar, both ? C::STAGE : C::STAGE / 2);
+                tma_load_3d(dst, &tm_k, 0, ask_head, ask_off + row0, bar);
+                if (both) tma_load_3d(dst + 16 * D, &tm_k, 0, ask_head, ask_off + row0 + 16, bar);
+                tma_load_3d(dst + C::HALF, &tm_v, 0, ask_head, ask_off + row0, bar);
+                if (both) tma_load_3d(dst + C::HALF + 16 * D, &tm_v, 0, ask_head, ask_off + row0 + 16, bar);
             }
-            if (lane < 2) {
-                const int64_t at = (o / kScaleRows + p.first_region + r + row0 / kScaleRows) * p.row_heads + h;
-                cp_async4(scales + ask_stage * 8 + lane * 4, (lane ? p.v_scale : p.k_scale) + at);
-            }
+            place = (ask_off / kScaleRows + row0 / kScaleRows + ask_region) * p.row_heads + ask_head;
             ask += C::SUBS;
         }
-        cp_commit();
         ask_stage = ask_stage + 1 == C::STAGES ? 0 : ask_stage + 1;
     };
 #pragma unroll
-    for (int i = 0; i < C::STAGES - 1; ++i) issue();
+    for (int i = 0; i < C::STAGES - 1; ++i) issue(scale_at[i]);
+    float next_k_scale = k_scales[scale_at[0]], next_v_scale = v_scales[scale_at[0]];
 
-    int tau = t0 + (sub - t0 % C::SUBS + C::SUBS) % C::SUBS, stage = 0;
-    for (int item = first_item; item < p.items && s_P[item] < t1; ++item) {
-        const int item_first = s_P[item], item_end = s_P[item + 1];
-        if (item_first == item_end) continue;
-        const int n = s_len[item], end = min(t1, item_end);
-
-        // the item's queries as fp16 fragments: columns are the heads of the KV group, lane (g, t) holds head g (+ 8)
-        uint32_t qf[NT][C::CHUNKS][8];
-        float f[NT][2];   // logits of heads 2t, 2t + 1 (+ 8) from the products, without the K scale
-        const uint16_t *q_item = p.q + ((int64_t)item * p.Hq + head * p.G) * D;
+    // an item's queries as they are: asked for while the item before is put together
+    uint32_t q_raw[NT][C::CHUNKS][8];
+    auto load_q = [&](int of) {
+        const uint16_t *from = p.q + ((int64_t)of * p.Hq + head * p.G) * D + t * (D / 4);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int h = nt * 8 + g;
-            uint4 x[C::CHUNKS][2];
-            uint32_t top = 0;
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int c = 0; c < C::CHUNKS; ++c)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    x[c][i] = make_uint4(0, 0, 0, 0);
-                    if (h < p.G) x[c][i] = *reinterpret_cast<const uint4 *>(q_item + h * D + c * 64 + t * 16 + i * 8);
-                    const uint32_t w[4] = {x[c][i].x, x[c][i].y, x[c][i].z, x[c][i].w};
+                    uint4 x = make_uint4(0, 0, 0, 0);
+                    if (nt * 8 + g < p.G) x = *reinterpret_cast<const uint4 *>(from + (nt * 8 + g) * D + c * 16 + i * 8);
+                    q_raw[nt][c][4 * i] = x.x;
+                    q_raw[nt][c][4 * i + 1] = x.y;
+                    q_raw[nt][c][4 * i + 2] = x.z;
+                    q_raw[nt][c][4 * i + 3] = x.w;
+                }
+    };
+    load_q(item);
+
+    bool ok = true;
+    while (true) {
+        const int end = min(t1, item_end);
+
+        // the item's queries as fp16 fragments: columns are the heads of the KV group, lane (g, t) holds head g (+ 8)
+        uint32_t qf[NT][C::CHUNKS][8];
+        float f[NT][2];   // logits of heads 2t, 2t + 1 (+ 8) from the products, without the K scale
 #pragma unroll
-                    for (int a = 0; a < 4; ++a) {
-                        const uint32_t l = w[a] & 0x7fffu, u = w[a] >> 16 & 0x7fffu;
+        for (int nt = 0; nt < NT; ++nt) {
+            uint32_t top2 = 0;
+#pragma unroll
+            for (int c = 0; c < C::CHUNKS; ++c)
+#pragma unroll
+                for (int a = 0; a < 8; ++a) top2 = __vmaxu2(top2, q_raw[nt][c][a] & 0x7fff7fffu);
+            uint32_t top = max(top2 & 0xffffu, top2 >> 16);
+            if (top >= 0x7f80) {   // infinities and NaN do not count
+                top = 0;
+#pragma unroll
+                for (int c = 0; c < C::CHUNKS; ++c)
+#pragma unroll
+                    for (int a = 0; a < 8; ++a) {
+                        const uint32_t l = q_raw[nt][c][a] & 0x7fffu, u = q_raw[nt][c][a] >> 16 & 0x7fffu;
                         top = max(top, max(l < 0x7f80 ? l : 0, u < 0x7f80 ? u : 0));
                     }
-                }
+            }
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
             // 2^e brings the largest magnitude to [2^7, 2^8); both 2^e and 2^-e are normal numbers
@@ -259,17 +370,9 @@ __global__ void __launch_bounds__(DecodeQCfg<D, HEADS, NT>::THREADS, 1) decode_q
 #pragma unroll
             for (int c = 0; c < C::CHUNKS; ++c)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t w[4] = {x[c][i].x, x[c][i].y, x[c][i].z, x[c][i].w};
-#pragma unroll
-                    for (int a = 0; a < 4; ++a) qf[nt][c][i * 4 + a] = f16x2(bf16lo(w[a]) * up, bf16hi(w[a]) * up);
-                }
+                for (int a = 0; a < 8; ++a) qf[nt][c][a] = f16x2(bf16lo(q_raw[nt][c][a]) * up, bf16hi(q_raw[nt][c][a]) * up);
             f[nt][0] = __shfl_sync(0xffffffffu, down, 8 * t) * p.sl2;
             f[nt][1] = __shfl_sync(0xffffffffu, down, 8 * t + 4) * p.sl2;
-        }
-        if (item + 1 < p.items && item_end < t1) {   // the next item's queries on their way
-            const char *next = reinterpret_cast<const char *>(p.q + (int64_t)(item + 1) * p.Hq * D);
-            for (int i = tid; i * 128 < p.Hq * D * 2; i += C::THREADS) prefetch_l2(next + i * 128);
         }
 
         float acc[NT][C::MT][4], ref[NT][2], sum[NT][2], v_top = 0.f, v_inv = 0.f;
@@ -282,50 +385,77 @@ __global__ void __launch_bounds__(DecodeQCfg<D, HEADS, NT>::THREADS, 1) decode_q
         }
 
         for (; tau < end; tau += C::SUBS) {
-            cp_wait<C::STAGES - 2>();
-            __syncwarp();
-            issue();
-            const unsigned char *tile = my_ring + stage * C::STAGE;
-            const float ks = my_scales[stage * 2], vs = my_scales[stage * 2 + 1];
-            stage = stage + 1 == C::STAGES ? 0 : stage + 1;
+            if (ok) ok = mbar_wait(bars + 8 * stage, parity, &s_abort, p.status, 10);
+            if (!__all_sync(0xffffffffu, ok)) {   // given up: what is written is incomplete, and reported
+                ok = false;
+                continue;
+            }
+            issue(scale_at[C::STAGES - 1]);
+            const unsigned char *tile = s_ring + (warp * C::STAGES + stage) * C::STAGE;
+            const float k_scale = next_k_scale, v_scale = next_v_scale;
+#pragma unroll
+            for (int i = 0; i + 1 < C::STAGES; ++i) scale_at[i] = scale_at[i + 1];
+            next_k_scale = k_scales[scale_at[0]];
+            next_v_scale = v_scales[scale_at[0]];
+            if (++stage == C::STAGES) { stage = 0; parity ^= 1; }
 
-            float s[NT][2][4];
+            const int rows = n - (tau - item_first) * kTile;   // of the tile, kTile or more unless it is the item's last
+            float x[kBlocks][NT][4];
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+                float s[NT][2][4];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[nt][0][i] = s[nt][1][i] = 0.f;
+                const unsigned char *k_tile = tile + b * 16 * D;
+#pragma unroll
+                for (int c = 0; c < C::CHUNKS; ++c) {
+                    // 128 channels: rows of 128 bytes, 16-byte piece i of row r at i ^ (r & 7); eight lanes read pieces 2t (or 2t + 1)
+                    // of two rows that differ in the lowest bit: all banks once.  64: rows of 64 bytes, piece i at i ^ (r / 2 & 3).
+                    const int at = D == 128 ? g * 128 + (((2 * t + c) ^ g) & 7) * 16 : g * 64 + ((t ^ (g >> 1)) & 3) * 16;
+                    const uint4 ka = *reinterpret_cast<const uint4 *>(k_tile + at), kb = *reinterpret_cast<const uint4 *>(k_tile + 8 * D + at);
+                    const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t a0 = e4m3x2_f16x2(wa[w] & 0xffffu), a2 = e4m3x2_f16x2(wa[w] >> 16);
+                        const uint32_t a1 = e4m3x2_f16x2(wb[w] & 0xffffu), a3 = e4m3x2_f16x2(wb[w] >> 16);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+                            mma_f16_16816(s[nt][w & 1], a0, a1, a2, a3, qf[nt][c][2 * w], qf[nt][c][2 * w + 1]);
+                    }
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[b][nt][i] = (s[nt][0][i] + s[nt][1][i]) * (f[nt][i & 1] * k_scale);
+            }
+            if (rows < kTile) {
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        if (16 * b + g >= rows) x[b][nt][0] = x[b][nt][1] = -INFINITY;
+                        if (16 * b + g + 8 >= rows) x[b][nt][2] = x[b][nt][3] = -INFINITY;
+                    }
+            }
+            float tops[NT][2];   // of this lane's keys
+            bool moves = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[nt][0][i] = s[nt][1][i] = 0.f;
+                for (int j = 0; j < 2; ++j) {
+                    tops[nt][j] = fmaxf(x[0][nt][j], x[0][nt][j + 2]);
 #pragma unroll
-            for (int c = 0; c < C::CHUNKS; ++c) {
-                const uint4 ka = *reinterpret_cast<const uint4 *>(tile + c * 512);
-                const uint4 kb = *reinterpret_cast<const uint4 *>(tile + (C::CHUNKS + c) * 512);
-                const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const uint32_t a0 = e4m3x2_f16x2(wa[w] & 0xffffu), a2 = e4m3x2_f16x2(wa[w] >> 16);
-                    const uint32_t a1 = e4m3x2_f16x2(wb[w] & 0xffffu), a3 = e4m3x2_f16x2(wb[w] >> 16);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma_f16_16816(s[nt][w & 1], a0, a1, a2, a3, qf[nt][c][2 * w], qf[nt][c][2 * w + 1]);
+                    for (int b = 1; b < kBlocks; ++b) tops[nt][j] = fmaxf(tops[nt][j], fmaxf(x[b][nt][j], x[b][nt][j + 2]));
+                    moves = moves || tops[nt][j] > ref[nt][j] + 4.f;
                 }
-            }
-            const int rows = n - (tau - item_first) * kTile;   // of the tile, 16 or more unless it is the item's last
-            bool moves = false;
-            float x[NT][4];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[nt][i] = (s[nt][0][i] + s[nt][1][i]) * (f[nt][i & 1] * ks);
-                if (rows < kTile) {
-                    if (g >= rows) x[nt][0] = x[nt][1] = -INFINITY;
-                    if (g + 8 >= rows) x[nt][2] = x[nt][3] = -INFINITY;
-                }
-                moves = moves || fmaxf(x[nt][0], x[nt][2]) > ref[nt][0] + 4.f || fmaxf(x[nt][1], x[nt][3]) > ref[nt][1] + 4.f;
-            }
             if (__any_sync(0xffffffffu, moves)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        float top = fmaxf(x[nt][j], x[nt][j + 2]);
+                        float top = tops[nt][j];
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
@@ -340,10 +470,10 @@ __global__ void __launch_bounds__(DecodeQCfg<D, HEADS, NT>::THREADS, 1) decode_q
                         }
                     }
             }
-            if (vs > v_top) {   // (all lanes alike)
-                const float shrink = v_top / vs;
-                v_top = vs;
-                v_inv = kLift / vs;
+            if (v_scale > v_top) {   // (all lanes alike)
+                const float shrink = v_top / v_scale;
+                v_top = v_scale;
+                v_inv = kLift / v_scale;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -351,131 +481,161 @@ __global__ void __launch_bounds__(DecodeQCfg<D, HEADS, NT>::THREADS, 1) decode_q
 #pragma unroll
                         for (int i = 0; i < 4; ++i) acc[nt][c][i] *= shrink;
             }
-            const float vf = vs * v_inv;
-            uint32_t head_b[NT][2], rest_b[NT][2];
+            const float vf = v_scale * v_inv;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int b = 0; b < kBlocks; ++b) {
+                uint32_t head_b[NT][2], rest_b[NT][2];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {   // keys g (i = 0) and g + 8
-                    const float p0 = fast_exp2(x[nt][2 * i] - ref[nt][0]), p1 = fast_exp2(x[nt][2 * i + 1] - ref[nt][1]);
-                    sum[nt][0] += p0;
-                    sum[nt][1] += p1;
-                    const uint32_t hi = f16x2(p0 * vf, p1 * vf);
-                    const float2 back = f16x2_f32(hi);
-                    head_b[nt][i] = movmatrix_trans(hi);
-                    rest_b[nt][i] = movmatrix_trans(f16x2(fmaf(p0, vf, -back.x), fmaf(p1, vf, -back.y)));
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {   // keys g (i = 0) and g + 8
+                        const float p0 = fast_exp2(x[b][nt][2 * i] - ref[nt][0]), p1 = fast_exp2(x[b][nt][2 * i + 1] - ref[nt][1]);
+                        sum[nt][0] += p0;
+                        sum[nt][1] += p1;
+                        const uint32_t hi = f16x2(p0 * vf, p1 * vf);
+                        const float2 back = f16x2_f32(hi);
+                        head_b[nt][i] = movmatrix_trans(hi);
+                        rest_b[nt][i] = movmatrix_trans(f16x2(fmaf(p0, vf, -back.x), fmaf(p1, vf, -back.y)));
+                    }
+                const unsigned char *v_tile = tile + C::HALF + b * 16 * D;
+                uint32_t vw[4][C::MT / 2];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int key = 2 * t + (i & 1) + 8 * (i >> 1);
+                    if (D == 128) {
+                        const uint4 x4 = *reinterpret_cast<const uint4 *>(v_tile + key * 128 + ((g ^ key) & 7) * 16);
+                        vw[i][0] = x4.x; vw[i][1] = x4.y; vw[i][C::MT / 2 - 2] = x4.z; vw[i][C::MT / 2 - 1] = x4.w;
+                    } else {
+                        const uint2 x2 = *reinterpret_cast<const uint2 *>(v_tile + key * 64 + (((g >> 1) ^ (key >> 1)) & 3) * 16 + (g & 1) * 8);
+                        vw[i][0] = x2.x; vw[i][1] = x2.y;
+                    }
                 }
-            uint32_t vw[4][C::MT / 2];
+                if (rows < kTile) {   // behind the rows in use: whatever lies there
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (D == 128) {
-                    const uint4 x4 = *reinterpret_cast<const uint4 *>(tile + kTile * D + i * 512);
-                    vw[i][0] = x4.x; vw[i][1] = x4.y; vw[i][C::MT / 2 - 2] = x4.z; vw[i][C::MT / 2 - 1] = x4.w;
-                } else {
-                    const uint2 x2 = *reinterpret_cast<const uint2 *>(tile + kTile * D + i * 256 - lane * 8);
-                    vw[i][0] = x2.x; vw[i][1] = x2.y;
+                    for (int i = 0; i < 4; ++i)
+                        if (16 * b + 2 * t + (i & 1) + 8 * (i >> 1) >= rows) {
+#pragma unroll
+                            for (int w = 0; w < C::MT / 2; ++w) vw[i][w] = 0;
+                        }
+                }
+#pragma unroll
+                for (int w = 0; w < C::MT / 2; ++w) {
+                    // channels 4w..4w+3 of this lane's stretch, two keys abreast
+                    const uint32_t l01 = __byte_perm(vw[0][w], vw[1][w], 0x5140), u01 = __byte_perm(vw[0][w], vw[1][w], 0x7362);
+                    const uint32_t l23 = __byte_perm(vw[2][w], vw[3][w], 0x5140), u23 = __byte_perm(vw[2][w], vw[3][w], 0x7362);
+                    const uint32_t a0 = e4m3x2_f16x2(l01 & 0xffffu), a1 = e4m3x2_f16x2(l01 >> 16);
+                    const uint32_t a2 = e4m3x2_f16x2(l23 & 0xffffu), a3 = e4m3x2_f16x2(l23 >> 16);
+                    const uint32_t b0 = e4m3x2_f16x2(u01 & 0xffffu), b1 = e4m3x2_f16x2(u01 >> 16);
+                    const uint32_t b2 = e4m3x2_f16x2(u23 & 0xffffu), b3 = e4m3x2_f16x2(u23 >> 16);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        mma_f16_16816(acc[nt][2 * w], a0, a1, a2, a3, head_b[nt][0], head_b[nt][1]);
+                        mma_f16_16816(acc[nt][2 * w + 1], b0, b1, b2, b3, head_b[nt][0], head_b[nt][1]);
+                        mma_f16_16816(acc[nt][2 * w], a0, a1, a2, a3, rest_b[nt][0], rest_b[nt][1]);
+                        mma_f16_16816(acc[nt][2 * w + 1], b0, b1, b2, b3, rest_b[nt][0], rest_b[nt][1]);
+                    }
                 }
             }
-#pragma unroll
-            for (int w = 0; w < C::MT / 2; ++w) {
-                // channels 4w..4w+3 of this lane's stretch, two keys abreast
-                const uint32_t l01 = __byte_perm(vw[0][w], vw[1][w], 0x5140), u01 = __byte_perm(vw[0][w], vw[1][w], 0x7362);
-                const uint32_t l23 = __byte_perm(vw[2][w], vw[3][w], 0x5140), u23 = __byte_perm(vw[2][w], vw[3][w], 0x7362);
-                const uint32_t a0 = e4m3x2_f16x2(l01 & 0xffffu), a1 = e4m3x2_f16x2(l01 >> 16);
-                const uint32_t a2 = e4m3x2_f16x2(l23 & 0xffffu), a3 = e4m3x2_f16x2(l23 >> 16);
-                const uint32_t b0 = e4m3x2_f16x2(u01 & 0xffffu), b1 = e4m3x2_f16x2(u01 >> 16);
-                const uint32_t b2 = e4m3x2_f16x2(u23 & 0xffffu), b3 = e4m3x2_f16x2(u23 >> 16);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    mma_f16_16816(acc[nt][2 * w], a0, a1, a2, a3, head_b[nt][0], head_b[nt][1]);
-                    mma_f16_16816(acc[nt][2 * w + 1], b0, b1, b2, b3, head_b[nt][0], head_b[nt][1]);
-                    mma_f16_16816(acc[nt][2 * w], a0, a1, a2, a3, rest_b[nt][0], rest_b[nt][1]);
-                    mma_f16_16816(acc[nt][2 * w + 1], b0, b1, b2, b3, rest_b[nt][0], rest_b[nt][1]);
-                }
-            }
+            __syncwarp();   // (the stage may be refilled from the next tile on)
         }
 
-        // the end of the item's part: sums over the lanes of a head, true units, then the tree over the head's warps
+        int next = item;   // (a list of items: empty ones are passed over)
+        if (item_end < t1) {
+            do ++next; while (s_P[next + 1] <= item_end);
+            load_q(next);
+        }
+        // the end of the item's part: sums over the lanes of a head, true units; then the warps of a head put their states
+        // into the ring stages that they have just read and share out the channels of the merged one
+        const bool whole = item_first >= t0 && item_end <= t1;
+        const int64_t slot_floats = partial_slot_floats(p.Hq, D);
+        float *slot = p.partials + (2 * (int64_t)cta + (item_first >= t0 ? 1 : 0)) * slot_floats;
+        float *item_out = whole ? p.out + (int64_t)item * p.Hq * D : slot;
         const float unit = v_top * (1.f / kLift);
+        const int free_stage = (stage + C::STAGES - 1) % C::STAGES;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 sum[nt][j] += __shfl_xor_sync(0xffffffffu, sum[nt][j], 4);
                 sum[nt][j] += __shfl_xor_sync(0xffffffffu, sum[nt][j], 8);
                 sum[nt][j] += __shfl_xor_sync(0xffffffffu, sum[nt][j], 16);
+            }
+            float weight[C::SUBS][2], top[2] = {ref[nt][0], ref[nt][1]}, all[2] = {sum[nt][0], sum[nt][1]};
+            const float *posted[C::SUBS];
+            weight[0][0] = weight[0][1] = 1.f;
+            if (C::SUBS > 1) {
+                float *post = reinterpret_cast<float *>(s_ring + (warp * C::STAGES + free_stage) * C::STAGE) + lane;
 #pragma unroll
-                for (int c = 0; c < C::MT; ++c) {
-                    acc[nt][c][j] *= unit;
-                    acc[nt][c][j + 2] *= unit;
+                for (int c = 0; c < C::MT; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) post[(c * 4 + i) * 32] = acc[nt][c][i] * unit;
+                if (g == 0) s_state[warp * 4 + t] = make_float4(top[0], top[1], all[0], all[1]);
+                if (lane == 0) s_free[warp] = free_stage;
+                head_barrier(head, C::SUBS * 32);
+                top[0] = top[1] = -1e30f;
+#pragma unroll
+                for (int i = 0; i < C::SUBS; ++i) {
+                    const float4 x = s_state[(i * HEADS + head) * 4 + t];
+                    weight[i][0] = x.x;
+                    weight[i][1] = x.y;
+                    top[0] = fmaxf(top[0], x.x);
+                    top[1] = fmaxf(top[1], x.y);
+                }
+                all[0] = all[1] = 0.f;
+#pragma unroll
+                for (int i = 0; i < C::SUBS; ++i) {
+                    const int w = i * HEADS + head;
+                    const float4 x = s_state[w * 4 + t];
+                    posted[i] = reinterpret_cast<const float *>(s_ring + (w * C::STAGES + s_free[w]) * C::STAGE) + lane;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) weight[i][j] = fast_exp2(weight[i][j] - top[j]);
+                    all[0] = fmaf(x.z, weight[i][0], all[0]);
+                    all[1] = fmaf(x.w, weight[i][1], all[1]);
                 }
             }
+            float times[2];
 #pragma unroll
-        for (int half = C::SUBS / 2; half >= 1; half >>= 1) {
-            if (sub >= half && sub < 2 * half) {
-                float *to = s_merge + (head * (C::SUBS / 2) + sub - half) * (C::STATE * 32) + lane;
+            for (int j = 0; j < 2; ++j) times[j] = !whole ? 1.f : all[j] > 0.f || all[j] != all[j] ? 1.f / all[j] : 0.f;
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    float *at = to + nt * (C::MT * 4 + 4) * 32;
-                    at[0] = ref[nt][0]; at[32] = ref[nt][1]; at[64] = sum[nt][0]; at[96] = sum[nt][1];
+            for (int c = 0; c < C::MT; ++c) {
+                if (C::SUBS > 1 && c % C::SUBS != sub) continue;
+                float m[4];
+                if (C::SUBS > 1) {
+                    m[0] = m[1] = m[2] = m[3] = 0.f;
 #pragma unroll
-                    for (int c = 0; c < C::MT; ++c)
+                    for (int i = 0; i < C::SUBS; ++i)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) at[(4 + c * 4 + i) * 32] = acc[nt][c][i];
+                        for (int x = 0; x < 4; ++x) m[x] = fmaf(posted[i][(c * 4 + x) * 32], weight[i][x & 1], m[x]);
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) m[x] = acc[nt][c][x] * unit;
                 }
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    if (nt * 8 + 2 * t + j < p.G)
+                        *reinterpret_cast<float2 *>(item_out + (int64_t)(head * p.G + nt * 8 + 2 * t + j) * D + g * (D / 8) + 2 * c) =
+                            make_float2(m[j] * times[j], m[j + 2] * times[j]);
             }
-            __syncthreads();
-            if (sub < half) {
-                const float *from = s_merge + (head * (C::SUBS / 2) + sub) * (C::STATE * 32) + lane;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const float *at = from + nt * (C::MT * 4 + 4) * 32;
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const float other = at[32 * j], now = fmaxf(fmaxf(ref[nt][j], other), -1e30f);
-                        const float mine = fast_exp2(ref[nt][j] - now), theirs = fast_exp2(other - now);
-                        ref[nt][j] = now;
-                        sum[nt][j] = sum[nt][j] * mine + at[64 + 32 * j] * theirs;
-#pragma unroll
-                        for (int c = 0; c < C::MT; ++c) {
-                            acc[nt][c][j] = acc[nt][c][j] * mine + at[(4 + c * 4 + j) * 32] * theirs;
-                            acc[nt][c][j + 2] = acc[nt][c][j + 2] * mine + at[(4 + c * 4 + j + 2) * 32] * theirs;
-                        }
-                    }
-                }
-            }
-            __syncthreads();
-        }
-
-        const bool whole = item_first >= t0 && item_end <= t1;
-        const int64_t slot_floats = partial_slot_floats(p.Hq, D);
-        float *slot = p.partials + (2 * (int64_t)cta + (item_first >= t0 ? 1 : 0)) * slot_floats;
-        if (sub == 0) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            if (!whole && g == 0 && sub == 0) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const int h = nt * 8 + 2 * t + j;
                     if (h >= p.G) continue;
-                    const int hq = head * p.G + h;
-                    const float times = whole ? (sum[nt][j] > 0.f || sum[nt][j] != sum[nt][j] ? 1.f / sum[nt][j] : 0.f) : 1.f;
-                    float *to = (whole ? p.out + ((int64_t)item * p.Hq + hq) * D : slot + (int64_t)hq * D) + g * (D / 8);
-#pragma unroll
-                    for (int c = 0; c < C::MT; c += 2)
-                        *reinterpret_cast<float4 *>(to + 2 * c) =
-                            make_float4(acc[nt][c][j] * times, acc[nt][c][j + 2] * times, acc[nt][c + 1][j] * times,
-                                        acc[nt][c + 1][j + 2] * times);
-                    if (!whole && g == 0) {
-                        slot[(int64_t)p.Hq * D + hq] = ref[nt][j];
-                        slot[(int64_t)p.Hq * (D + 1) + hq] = sum[nt][j];
-                    }
+                    slot[(int64_t)p.Hq * D + head * p.G + h] = top[j];
+                    slot[(int64_t)p.Hq * (D + 1) + head * p.G + h] = all[j];
                 }
+            }
+            if (C::SUBS > 1) {   // the stages go back to the copies
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                head_barrier(head, C::SUBS * 32);
+            }
         }
         if (!whole) {
             __syncthreads();
-            // the CTAs that have a part of the item, in order: tile u belongs to CTA ((u + 1) * ctas - 1) / total
-            const int c_first = (int)(((int64_t)(item_first + 1) * ctas - 1) / total);
-            const int c_last = (int)(((int64_t)item_end * ctas - 1) / total);
+            if (!pieces) {   // the CTAs that have a part of the item, in order: tile u belongs to CTA ((u + 1) * ctas - 1) / total
+                c_first = (int)(((int64_t)(item_first + 1) * ctas - 1) / total);
+                c_last = (int)(((int64_t)item_end * ctas - 1) / total);
+            }
             if (tid == 0) {
                 __threadfence();
                 s_last = atomicAdd(p.tickets + item, 1) == c_last - c_first;
@@ -486,6 +646,7 @@ __global__ void __launch_bounds__(DecodeQCfg<D, HEADS, NT>::THREADS, 1) decode_q
                 for (int e = tid; e < p.Hq * D; e += C::THREADS) {
                     const int hq = e / D;
                     float m = -1e30f, o = 0.f, l = 0.f;
+#pragma unroll 4
                     for (int c = c_first; c <= c_last; ++c) {
                         const float *from = p.partials + (2 * (int64_t)c + (c == c_first ? 1 : 0)) * slot_floats;
                         const float cm = __ldcg(from + (int64_t)p.Hq * D + hq), cl = __ldcg(from + (int64_t)p.Hq * (D + 1) + hq);
@@ -500,31 +661,54 @@ __global__ void __launch_bounds__(DecodeQCfg<D, HEADS, NT>::THREADS, 1) decode_q
                 if (tid == 0) p.tickets[item] = 0;
             }
         }
+        if (item_end >= t1) break;
+        item = next;
+        item_first = item_end;
+        item_end = s_P[item + 1];
+        n = s_len[item];
     }
-    cp_wait<0>();
+    // a wait that gave up: copies in flight get their time before the block's memory goes
+    if (s_abort)
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
 }
 
+// e4m3 [rows, heads, D] as a 3-D tensor of bytes (D, heads, rows); a box is 16 rows of one head.
+int make_map(CUtensorMap *tm, const void *base, int D, int heads, int64_t rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) { set_last_cuda_error(cudaErrorSymbolNotFound); return AIRCACHE_ERR_CUDA; }
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)rows};
+    const cuuint64_t strides[2] = {(cuuint64_t)D, (cuuint64_t)heads * D};
+    const cuuint32_t box[3] = {(cuuint32_t)D, 1, 16}, estr[3] = {1, 1, 1};
+    const CUresult rc = fn(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(base), dims, strides, box, estr,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (rc != CUDA_SUCCESS) { set_last_cuda_error(cudaErrorInvalidValue); return AIRCACHE_ERR_CUDA; }
+    return AIRCACHE_OK;
+}
+
+struct Maps { CUtensorMap k, v; };
+
 template <int D, int HEADS, int NT>
-int launch_t(const DecodeQParams &p, int ctas, int dev, cudaStream_t st) {
+int launch_t(const Maps &m, const DecodeQParams &p, int ctas, int dev, cudaStream_t st) {
     using C = DecodeQCfg<D, HEADS, NT>;
     static std::atomic<uint64_t> allowed[kMaxDevices];
     const int rc = allow_shared_memory((const void *)decode_quantized_kernel<D, HEADS, NT>, C::SMEM, dev, allowed);
     if (rc) return rc;
-    return launch_dependent(decode_quantized_kernel<D, HEADS, NT>, dim3(ctas), dim3(C::THREADS), C::SMEM, st, p);
+    return launch_dependent(decode_quantized_kernel<D, HEADS, NT>, dim3(ctas), dim3(C::THREADS), C::SMEM, st, m.k, m.v, p);
 }
 
 template <int D, int HEADS>
-int launch_g(const DecodeQParams &p, int ctas, int dev, cudaStream_t st) {
-    return p.G > 8 ? launch_t<D, HEADS, 2>(p, ctas, dev, st) : launch_t<D, HEADS, 1>(p, ctas, dev, st);
+int launch_g(const Maps &m, const DecodeQParams &p, int ctas, int dev, cudaStream_t st) {
+    return p.G > 8 ? launch_t<D, HEADS, 2>(m, p, ctas, dev, st) : launch_t<D, HEADS, 1>(m, p, ctas, dev, st);
 }
 
 template <int D>
-int launch_d(const DecodeQParams &p, int heads, int ctas, int dev, cudaStream_t st) {
+int launch_d(const Maps &m, const DecodeQParams &p, int heads, int ctas, int dev, cudaStream_t st) {
     switch (heads) {
-        case 1: return launch_g<D, 1>(p, ctas, dev, st);
-        case 2: return launch_g<D, 2>(p, ctas, dev, st);
-        case 4: return launch_g<D, 4>(p, ctas, dev, st);
-        case 8: return launch_g<D, 8>(p, ctas, dev, st);
+        case 1: return launch_g<D, 1>(m, p, ctas, dev, st);
+        case 2: return launch_g<D, 2>(m, p, ctas, dev, st);
+        case 4: return launch_g<D, 4>(m, p, ctas, dev, st);
+        case 8: return launch_g<D, 8>(m, p, ctas, dev, st);
         default: return AIRCACHE_ERR_UNSUPPORTED;
     }
 }
@@ -538,8 +722,6 @@ int launch_decode_quantized(const aircache_shape_t *s, const aircache_quantized_
     if (rc) return rc;
     const int ctas = sms < kMaxDecodeCtas ? sms : kMaxDecodeCtas;
     DecodeQParams p = {};
-    p.k = static_cast<const char *>(c->k);
-    p.v = static_cast<const char *>(c->v);
     p.k_scale = c->k_scale;
     p.v_scale = c->v_scale;
     p.offsets = c->offsets;
@@ -548,6 +730,7 @@ int launch_decode_quantized(const aircache_shape_t *s, const aircache_quantized_
     p.out = out;
     p.tickets = ws_ptr<int32_t>(ws, w.tickets);
     p.partials = ws_ptr<float>(ws, w.partials);
+    p.status = ws_ptr<uint32_t>(ws, w.status);
     p.rows = c->total_rows;
     p.scale_blocks = c->scale_blocks;
     p.first_region = c->first_region;
@@ -564,7 +747,10 @@ int launch_decode_quantized(const aircache_shape_t *s, const aircache_quantized_
         heads = 1;
     }
     p.Hq = heads * p.G;
-    return s->head_dim == 64 ? launch_d<64>(p, heads, ctas, dev, st) : launch_d<128>(p, heads, ctas, dev, st);
+    Maps m;
+    if ((rc = make_map(&m.k, c->k, s->head_dim, p.row_heads, c->total_rows))) return rc;
+    if ((rc = make_map(&m.v, c->v, s->head_dim, p.row_heads, c->total_rows))) return rc;
+    return s->head_dim == 64 ? launch_d<64>(m, p, heads, ctas, dev, st) : launch_d<128>(m, p, heads, ctas, dev, st);
 }
 
 }  // namespace aircache

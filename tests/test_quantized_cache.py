@@ -238,12 +238,13 @@ LENGTHS = {
     "edges": [0, 1, 15, 16, 17, 63, 64, 65, 0, 127, 128, 129, 300],
     "long": [5000, 3],
     "many": [(7 * i) % 50 for i in range(200)],
+    "most": [(5 * i) % 40 for i in range(1792)],   # as many regions as a shape may have
 }
 
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("H,d", [(1, 64), (1, 128), (2, 128), (4, 64), (8, 128)])
-@pytest.mark.parametrize("lens", ["one", "edges", "many"])
+@pytest.mark.parametrize("lens", ["one", "edges", "many", "most"])
 def test_quantize(lens, H, d):
     c = Cache(LENGTHS[lens], H, d, slack=2, seed=H)
     want = c.expected()
@@ -301,6 +302,12 @@ def test_decode(lens, H, G, d):
     again = torch.full_like(out, float("nan"))
     ac.aircache_decode_attn_quantized(c.sh, c.cache8, q, again, c.ws)
     assert torch.equal(out, again)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H,G,d", [(1, 7, 64), (2, 9, 64), (4, 2, 128)])
+def test_decode_of_as_many_regions_as_there_may_be(H, G, d):
+    test_decode("most", H, G, d)
 
 
 @pytest.mark.gpu
