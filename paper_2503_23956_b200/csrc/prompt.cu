@@ -54,7 +54,7 @@ struct PromptCfg {
     static constexpr int HALF = kKeys * 128;             // of 64 channels of it
     static constexpr int SLOTS = D == 128 ? 5 : 8;
     static constexpr int SMEM = 1024 + (2 + SLOTS) * TILE;
-    static constexpr int THREADS = 320;
+    static constexpr int THREADS = 384;                  // three warpgroups of 168 registers a thread, moved below
 };
 
 // PV: bf16 x bf16 -> fp32, A from tensor memory (K-major), B from shared memory with N contiguous
@@ -86,29 +86,58 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return r;
 }
 
+// Asks for a block of this grid that has not started yet; the answer (16 bytes) is counted on an mbarrier.
+__device__ __forceinline__ void take_block(uint32_t answer, uint32_t bar) {
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
+                 ::"r"(answer), "r"(bar) : "memory");
+}
+// The block of the answer, or -1 if there is none left.
+__device__ __forceinline__ int taken_block(uint32_t answer) {
+    uint32_t ok, x;
+    asm volatile(
+        "{\n.reg .b128 r;\n.reg .pred p;\n.reg .b32 y, z, w;\n"
+        "ld.shared.b128 r, [%2];\n"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n"
+        "mov.b32 %1, 0;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, y, z, w}, r;\n}\n"
+        : "=r"(ok), "=r"(x) : "r"(answer) : "memory");
+    return ok ? (int)x : -1;
+}
+
+// A block's unit of work: two row tiles of one sequence and KV head.
+struct Unit {
+    int q0, n_q, k0, n_k;   // the sequence's rows
+    int first, group;       // first token of the first tile; KV head, -1: no more units
+    int tiles[2];           // key tiles of each row tile
+};
+
 template <int D>
 __global__ void __launch_bounds__(PromptCfg<D>::THREADS, 1)
 prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
               const __grid_constant__ CUtensorMap tm_v, const PromptParams p) {
     using C = PromptCfg<D>;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ uint64_t s_bars[1 + 2 * C::SLOTS + 6];
+    __shared__ uint64_t s_bars[2 + 2 * C::SLOTS + 6 + 5];
+    __shared__ __align__(16) uint32_t s_answer[4];
+    __shared__ Unit s_unit[2];
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_abort;
-    __shared__ int s_unit[5];   // sequence's q0, n_q, k0, n_k, first token
     const uint32_t smem = (smem_u32(smem_raw) + 1023) & ~1023u;
     const uint32_t q_smem = smem, ring = smem + 2 * C::TILE;
     const uint32_t bars = smem_u32(s_bars);
-    const uint32_t q_full = bars, kv_full = bars + 8, kv_empty = kv_full + 8 * C::SLOTS, s_full = kv_empty + 8 * C::SLOTS,
-                   p_full = s_full + 16, o_done = p_full + 16;
+    const uint32_t q_full = bars, q_empty = bars + 8, kv_full = bars + 16, kv_empty = kv_full + 8 * C::SLOTS,
+                   s_full = kv_empty + 8 * C::SLOTS, p_full = s_full + 16, o_done = p_full + 16, unit_full = o_done + 16,
+                   unit_empty = unit_full + 16, answered = unit_empty + 16;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int group = blockIdx.x % p.n_kv_heads, TPT = p.tokens_per_tile;
+    const int TPT = p.tokens_per_tile;
     uint32_t *status = &g_prompt_status;
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (warp == 9) tmem_alloc(smem_u32(&s_tmem), 512);
     if (warp == 8 && lane == 0) {
         mbar_init(q_full, 1);
+        mbar_init(q_empty, 1);
         for (int i = 0; i < C::SLOTS; ++i) {
             mbar_init(kv_full + 8 * i, 1);
             mbar_init(kv_empty + 8 * i, 1);
@@ -117,242 +146,302 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             mbar_init(s_full + 8 * i, 1);
             mbar_init(p_full + 8 * i, 128);
             mbar_init(o_done + 8 * i, 1);
+            mbar_init(unit_full + 8 * i, 1);
+            mbar_init(unit_empty + 8 * i, 9);   // a lane of each warp that reads a unit
         }
+        mbar_init(answered, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_abort = 0;
-    }
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (warp == 0) {   // the block's unit: counted from the last one back
-        int unit = p.units - 1 - (int)(blockIdx.x / p.n_kv_heads);
-        if (lane < 5) s_unit[lane] = 0;   // (a block of a grid larger than the units: no tokens)
-        __syncwarp();
-        int before = 0;
-        for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
-            const int s = s0 + lane;
-            int q0 = 0, n_q = 0, n = 0;
-            if (s < p.n_seqs) {
-                q0 = min(max(p.q_offsets[s], 0), p.q_tokens);
-                n_q = min(max(p.q_offsets[s + 1], q0), p.q_tokens) - q0;
-                n = (n_q + 2 * TPT - 1) / (2 * TPT);
-            }
-            int incl = n;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int x = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += x;
-            }
-            const int mine = before + incl - n;
-            if (unit >= mine && unit < mine + n) {
-                const int k0 = min(max(p.k_offsets[s], 0), p.k_tokens);
-                s_unit[0] = q0;
-                s_unit[1] = n_q;
-                s_unit[2] = k0;
-                s_unit[3] = min(max(p.k_offsets[s + 1], k0), p.k_tokens) - k0;
-                s_unit[4] = (unit - mine) * 2 * TPT;
-            }
-            before += __shfl_sync(0xffffffffu, incl, 31);
-            if (before > unit) break;
-        }
+        asm volatile("prefetch.tensormap [%0];\nprefetch.tensormap [%1];\nprefetch.tensormap [%2];"
+                     ::"l"(&tm_q), "l"(&tm_k), "l"(&tm_v) : "memory");
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t tmem = s_tmem;
-    const int q0 = s_unit[0], n_q = s_unit[1], k0 = s_unit[2], n_k = s_unit[3], first = s_unit[4];
-    int tiles[2];   // key tiles of each row tile
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int t0 = first + i * TPT, last = min(t0 + TPT, n_q) - 1;
-        const int seen = t0 >= n_q ? 0 : min(n_k, p.causal ? n_k - n_q + last + 1 : n_k);
-        tiles[i] = seen <= 0 ? 0 : (seen + kKeys - 1) / kKeys;
-    }
-    const int n_tiles = max(tiles[0], tiles[1]);
+    // The unit of turn `it`, as the producer has left it.
+    auto next_unit = [&](int it, Unit &u) {
+        const bool ok = __all_sync(0xffffffffu, mbar_wait(unit_full + 8 * (it & 1), it >> 1 & 1, &s_abort, status, 8));
+        if (!ok) return false;
+        u = s_unit[it & 1];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(unit_empty + 8 * (it & 1));
+        return u.group >= 0;
+    };
 
-    if (warp == 8) {
-        if (lane == 0 && n_tiles > 0) {
-            const int rows = TPT * p.G;
-            const int n_row_tiles = tiles[1] > 0 ? 2 : 1;   // (the second has keys whenever it has tokens and the first has)
-            mbar_expect_tx(q_full, 2 * C::HALVES * 128 * rows);
-            for (int i = 0; i < 2; ++i)
-                for (int h = 0; h < C::HALVES; ++h)   // (the second tile again where there is none: the barrier counts both)
-                    tma_load_3d(q_smem + i * C::TILE + h * C::HALF, &tm_q, h * 64, group * p.G,
-                                q0 + first + (i < n_row_tiles ? i : 0) * TPT, q_full);
-            int slot = 0, phase = 0;
-            for (int c = 0; c < 2 * n_tiles; ++c) {
-                if (c >= C::SLOTS && !mbar_wait(kv_empty + 8 * slot, phase ^ 1, &s_abort, status, 1)) break;
-                mbar_expect_tx(kv_full + 8 * slot, C::TILE);
-                for (int h = 0; h < C::HALVES; ++h)
-                    tma_load_3d(ring + slot * C::TILE + h * C::HALF, c & 1 ? &tm_v : &tm_k, h * 64, group, k0 + (c >> 1) * kKeys,
-                                kv_full + 8 * slot);
-                if (++slot == C::SLOTS) { slot = 0; phase ^= 1; }
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (warp == 8) {
+            int block = blockIdx.x, slot = 0, loaded = 0, full_units = 0;
+            bool ok = true;
+            for (int it = 0; ok; ++it) {
+                Unit u = {};
+                u.group = -1;
+                if (block >= 0) {   // the block's unit: counted from the last one back
+                    const int unit = p.units - 1 - block / p.n_kv_heads;
+                    u.group = block % p.n_kv_heads;
+                    int before = 0;
+                    for (int s0 = 0; s0 < p.n_seqs && before <= unit; s0 += 32) {
+                        const int s = s0 + lane;
+                        int q0 = 0, n_q = 0, n = 0;
+                        if (s < p.n_seqs) {
+                            q0 = min(max(p.q_offsets[s], 0), p.q_tokens);
+                            n_q = min(max(p.q_offsets[s + 1], q0), p.q_tokens) - q0;
+                            n = (n_q + 2 * TPT - 1) / (2 * TPT);
+                        }
+                        int incl = n;
+#pragma unroll
+                        for (int o = 1; o < 32; o <<= 1) {
+                            const int x = __shfl_up_sync(0xffffffffu, incl, o);
+                            if (lane >= o) incl += x;
+                        }
+                        const int mine = before + incl - n;
+                        const unsigned who = __ballot_sync(0xffffffffu, unit >= mine && unit < mine + n);
+                        if (who) {
+                            const int src = __ffs(who) - 1, at = s0 + src;
+                            u.q0 = __shfl_sync(0xffffffffu, q0, src);
+                            u.n_q = __shfl_sync(0xffffffffu, n_q, src);
+                            u.first = (unit - __shfl_sync(0xffffffffu, mine, src)) * 2 * TPT;
+                            u.k0 = min(max(p.k_offsets[at], 0), p.k_tokens);
+                            u.n_k = min(max(p.k_offsets[at + 1], u.k0), p.k_tokens) - u.k0;
+                        }
+                        before += __shfl_sync(0xffffffffu, incl, 31);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {   // (a block of a grid larger than the units has no tokens: n_q = 0)
+                        const int t0 = u.first + i * TPT, last = min(t0 + TPT, u.n_q) - 1;
+                        const int seen = t0 >= u.n_q ? 0 : min(u.n_k, p.causal ? u.n_k - u.n_q + last + 1 : u.n_k);
+                        u.tiles[i] = seen <= 0 ? 0 : (seen + kKeys - 1) / kKeys;
+                    }
+                }
+                if (it >= 2) ok = mbar_wait(unit_empty + 8 * (it & 1), (it >> 1) + 1 & 1, &s_abort, status, 9);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                if (lane == 0) {
+                    s_unit[it & 1] = u;
+                    mbar_arrive(unit_full + 8 * (it & 1));
+                }
+                if (block < 0) break;
+                if (lane == 0) {
+                    mbar_expect_tx(answered, 16);
+                    take_block(smem_u32(s_answer), answered);
+                    const int n_tiles = max(u.tiles[0], u.tiles[1]);
+                    if (n_tiles > 0) {
+                        if (full_units > 0) ok = mbar_wait(q_empty, full_units + 1 & 1, &s_abort, status, 1);
+                        if (ok) {
+                            const int n_rows = u.tiles[1] > 0 ? 2 : 1;   // (the second tile has keys whenever it has tokens and the first has)
+                            mbar_expect_tx(q_full, n_rows * C::HALVES * 128 * TPT * p.G);
+                            for (int i = 0; i < n_rows; ++i)
+                                for (int h = 0; h < C::HALVES; ++h)
+                                    tma_load_3d(q_smem + i * C::TILE + h * C::HALF, &tm_q, h * 64, u.group * p.G, u.q0 + u.first + i * TPT, q_full);
+                        }
+                        for (int c = 0; ok && c < 2 * n_tiles; ++c, ++loaded) {
+                            if (loaded >= C::SLOTS) ok = mbar_wait(kv_empty + 8 * slot, loaded / C::SLOTS + 1 & 1, &s_abort, status, 1);
+                            if (!ok) break;
+                            mbar_expect_tx(kv_full + 8 * slot, C::TILE);
+                            for (int h = 0; h < C::HALVES; ++h)
+                                tma_load_3d(ring + slot * C::TILE + h * C::HALF, c & 1 ? &tm_v : &tm_k, h * 64, u.group, u.k0 + (c >> 1) * kKeys,
+                                            kv_full + 8 * slot);
+                            if (++slot == C::SLOTS) slot = 0;
+                        }
+                        ++full_units;
+                    }
+                }
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                ok = __all_sync(0xffffffffu, mbar_wait(answered, it & 1, &s_abort, status, 9));
+                if (!ok) break;
+                block = taken_block(smem_u32(s_answer));
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the next answer goes to the same place)
+                __syncwarp();
             }
-        }
-    } else if (warp == 9) {
-        if (n_tiles > 0) {
+        } else if (warp == 9) {
             const uint32_t idesc_s = umma_idesc_bf16(128, kKeys);
             const uint32_t idesc_o = umma_idesc_bf16(128, D) | 1u << 16;   // B with N contiguous
-            bool ok = __all_sync(0xffffffffu, mbar_wait(q_full, 0, &s_abort, status, 2));
-            int seen = 0;   // tiles of the ring whose arrival has been waited for
-            auto arrived = [&](int c) {
-                for (; ok && seen <= c; ++seen)
-                    ok = __all_sync(0xffffffffu, mbar_wait(kv_full + 8 * (seen % C::SLOTS), seen / C::SLOTS & 1, &s_abort, status, 3));
-                tc_fence_after();
-            };
-            auto scores = [&](int i, int j) {   // S_i = Q_i K_j^T
-                if (elect_one()) {
-                    const uint32_t k_tile = ring + (2 * j % C::SLOTS) * C::TILE;
+            bool ok = true;
+            int base = 0, seen = 0, full_units = 0;   // tiles of the ring: in front of this unit, waited for
+            int done[2] = {0, 0};                     // key tiles of either row tile in front of this unit
+            Unit u;
+            for (int it = 0; ok && next_unit(it, u); ++it) {
+                const int n_tiles = max(u.tiles[0], u.tiles[1]);
+                if (n_tiles == 0) continue;
+                auto arrived = [&](int c) {
+                    for (; ok && seen <= base + c; ++seen)
+                        ok = __all_sync(0xffffffffu, mbar_wait(kv_full + 8 * (seen % C::SLOTS), seen / C::SLOTS & 1, &s_abort, status, 3));
+                    tc_fence_after();
+                };
+                auto scores = [&](int i, int j) {   // S_i = Q_i K_j^T
+                    if (elect_one()) {
+                        const uint32_t k_tile = ring + ((base + 2 * j) % C::SLOTS) * C::TILE;
 #pragma unroll
-                    for (int s = 0; s < D / 16; ++s)
-                        umma_bf16(tmem + i * kKeys, umma_desc_sw128(q_smem + i * C::TILE + (s >> 2) * C::HALF + (s & 3) * 32),
-                                  umma_desc_sw128(k_tile + (s >> 2) * C::HALF + (s & 3) * 32), idesc_s, s > 0);
-                    umma_commit(s_full + 8 * i);
-                }
-                __syncwarp();
-            };
-            auto release = [&](int c) {
-                if (elect_one()) umma_commit(kv_empty + 8 * (c % C::SLOTS));
-                __syncwarp();
-            };
-            arrived(0);
-            for (int i = 0; i < 2; ++i)
-                if (ok && tiles[i] > 0) scores(i, 0);
-            if (ok) release(0);
-            for (int j = 0; ok && j < n_tiles; ++j) {
-                const uint32_t v_tile = ring + ((2 * j + 1) % C::SLOTS) * C::TILE;
-                arrived(2 * j + 1);
-                if (!ok) break;
-                const int rows = n_k - j * kKeys;
-                if (rows < kKeys) {   // keys behind the sequence's last: zeros
-                    for (int e = lane; e < (kKeys - rows) * C::HALVES * 8; e += 32) {
-                        const uint32_t at = v_tile + (e / ((kKeys - rows) * 8)) * C::HALF + rows * 128 + e % ((kKeys - rows) * 8) * 16;
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
+                        for (int s = 0; s < D / 16; ++s)
+                            umma_bf16(tmem + i * kKeys, umma_desc_sw128(q_smem + i * C::TILE + (s >> 2) * C::HALF + (s & 3) * 32),
+                                      umma_desc_sw128(k_tile + (s >> 2) * C::HALF + (s & 3) * 32), idesc_s, s > 0);
+                        umma_commit(s_full + 8 * i);
                     }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
-                }
-                for (int i = 0; i < 2 && ok; ++i) {
-                    if (j < tiles[i]) {
-                        ok = __all_sync(0xffffffffu, mbar_wait(p_full + 8 * i, j & 1, &s_abort, status, 4));
-                        if (!ok) break;
-                        tc_fence_after();
-                        if (elect_one()) {
-#pragma unroll
-                            for (int s = 0; s < kKeys / 16; ++s)
-                                umma_bf16_ts(tmem + 256 + i * 128, tmem + i * kKeys + s * 8, umma_desc_rows_are_k(v_tile + s * 2048),
-                                             idesc_o, j > 0 || s > 0);
-                            umma_commit(o_done + 8 * i);
+                };
+                auto commit = [&](uint32_t bar) {
+                    if (elect_one()) umma_commit(bar);
+                    __syncwarp();
+                };
+                auto release = [&](int c) { commit(kv_empty + 8 * ((base + c) % C::SLOTS)); };
+                ok = __all_sync(0xffffffffu, mbar_wait(q_full, full_units & 1, &s_abort, status, 2));
+                ++full_units;
+                arrived(0);
+                if (!ok) break;
+                for (int i = 0; i < 2; ++i)
+                    if (u.tiles[i] > 0) scores(i, 0);
+                release(0);
+                if (n_tiles == 1) commit(q_empty);
+                for (int j = 0; ok && j < n_tiles; ++j) {
+                    const uint32_t v_tile = ring + ((base + 2 * j + 1) % C::SLOTS) * C::TILE;
+                    arrived(2 * j + 1);
+                    if (!ok) break;
+                    const int rows = u.n_k - j * kKeys;
+                    if (rows < kKeys) {   // keys behind the sequence's last: zeros
+                        for (int e = lane; e < (kKeys - rows) * C::HALVES * 8; e += 32) {
+                            const uint32_t at = v_tile + (e / ((kKeys - rows) * 8)) * C::HALF + rows * 128 + e % ((kKeys - rows) * 8) * 16;
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
                         }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
                     }
-                    if (i == 1) release(2 * j + 1);
-                    if (j + 1 < tiles[i]) {
-                        arrived(2 * j + 2);
-                        if (ok) scores(i, j + 1);
+                    for (int i = 0; i < 2 && ok; ++i) {
+                        if (j < u.tiles[i]) {
+                            ok = __all_sync(0xffffffffu, mbar_wait(p_full + 8 * i, done[i] + j & 1, &s_abort, status, 4));
+                            if (!ok) break;
+                            tc_fence_after();
+                            if (elect_one()) {
+#pragma unroll
+                                for (int s = 0; s < kKeys / 16; ++s)
+                                    umma_bf16_ts(tmem + 256 + i * 128, tmem + i * kKeys + s * 8, umma_desc_rows_are_k(v_tile + s * 2048),
+                                                 idesc_o, j > 0 || s > 0);
+                                umma_commit(o_done + 8 * i);
+                            }
+                            __syncwarp();
+                        }
+                        if (i == 1) release(2 * j + 1);
+                        if (j + 1 < u.tiles[i]) {
+                            arrived(2 * j + 2);
+                            if (ok) scores(i, j + 1);
+                        }
                     }
+                    if (ok && j + 1 < n_tiles) release(2 * j + 2);
+                    if (ok && j + 2 == n_tiles) commit(q_empty);   // (the unit's last scores are issued)
                 }
-                if (ok && j + 1 < n_tiles) release(2 * j + 2);
+                base += 2 * n_tiles;
+                done[0] += u.tiles[0];
+                done[1] += u.tiles[1];
             }
         }
     } else {
-        const int i = warp >> 2, row = tid & 127, n = tiles[i];
-        const int token = first + i * TPT + row / p.G;
-        const bool used = row < TPT * p.G && token < n_q;
-        const int t0 = first + i * TPT;
-        const int limit = !used ? 0 : max(0, min(n_k, p.causal ? n_k - n_q + token + 1 : n_k));
-        const int all_see = p.causal ? n_k - n_q + t0 + 1 : n_k;   // keys that every token of the tile sees
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        const int i = warp >> 2, row = tid & 127;
+        const int row_token = row / p.G, row_head = row - row_token * p.G;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;          // 32 * (warp % 4) tensor-memory lanes
         const uint32_t s_at = tmem + i * kKeys + lanes, o_at = tmem + 256 + i * 128 + lanes;
-        float ref = -1e30f;
-        float2 sum = make_float2(0.f, 0.f);
         bool ok = true;
-        for (int j = 0; j < n; ++j) {
-            ok = mbar_wait(s_full + 8 * i, j & 1, &s_abort, status, 5);
-            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-            tc_fence_after();
-            uint32_t x[4][32];
+        int done = 0;   // key tiles in front of this unit
+        Unit u;
+        for (int it = 0; ok && next_unit(it, u); ++it) {
+            const int n = u.tiles[i], t0 = u.first + i * TPT, token = t0 + row_token;
+            const bool used = row_token < TPT && token < u.n_q;
+            const int limit = !used ? 0 : max(0, min(u.n_k, p.causal ? u.n_k - u.n_q + token + 1 : u.n_k));
+            const int all_see = min(u.n_k, p.causal ? u.n_k - u.n_q + t0 + 1 : u.n_k);   // keys that every token of the tile sees
+            float ref = -1e30f;
+            float2 sum = make_float2(0.f, 0.f);
+            for (int j = 0; j < n; ++j) {
+                ok = mbar_wait(s_full + 8 * i, done + j & 1, &s_abort, status, 5);
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                tc_fence_after();
+                uint32_t x[4][32];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32_issue(s_at + c * 32, x[c]);
+                for (int c = 0; c < 4; ++c) tmem_ld32_issue(s_at + c * 32, x[c]);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld_wait(x[c]);
-            if ((j + 1) * kKeys > all_see || (j + 1) * kKeys > n_k) {
-                const int left = limit - j * kKeys;
+                for (int c = 0; c < 4; ++c) tmem_ld_wait(x[c]);
+                if ((j + 1) * kKeys > all_see) {
+                    const int left = limit - j * kKeys;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (c * 32 + e >= left) x[c][e] = 0xff800000u;
+                }
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (c * 32 + e >= left) x[c][e] = 0xff800000u;
-            }
-            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-#pragma unroll
-                for (int e = 0; e < 32; e += 2)
-                    top[c] = fmaxf(top[c], fmaxf(__uint_as_float(x[c][e]), __uint_as_float(x[c][e + 1])));
-            const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.sl2;
-            const bool moves = now > ref + 8.f;
-            if (__any_sync(0xffffffffu, moves)) {
-                const float to = moves ? now : ref, shrink = fast_exp2(ref - to);
-                ref = to;
-                sum.x *= shrink;
-                sum.y *= shrink;
-                if (j > 0) {   // O_i of the key tiles before: its last product has to be done
-                    ok = mbar_wait(o_done + 8 * i, (j - 1) & 1, &s_abort, status, 6);
-                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                    tc_fence_after();
+                    for (int e = 0; e < 32; e += 2)
+                        top[c] = fmaxf(top[c], fmaxf(__uint_as_float(x[c][e]), __uint_as_float(x[c][e + 1])));
+                const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.sl2;
+                const bool moves = now > ref + 8.f;
+                if (__any_sync(0xffffffffu, moves)) {
+                    const float to = moves ? now : ref, shrink = fast_exp2(ref - to);
+                    ref = to;
+                    sum.x *= shrink;
+                    sum.y *= shrink;
+                    if (j > 0) {   // O_i of the key tiles before: its last product has to be done
+                        ok = mbar_wait(o_done + 8 * i, done + j - 1 & 1, &s_abort, status, 6);
+                        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                        tc_fence_after();
 #pragma unroll 1
-                    for (int c = 0; c < D / 32; ++c) {
-                        uint32_t o[32];
-                        tmem_ld32_issue(o_at + c * 32, o);
-                        tmem_ld_wait(o);
+                        for (int c = 0; c < D / 32; ++c) {
+                            uint32_t o[32];
+                            tmem_ld32_issue(o_at + c * 32, o);
+                            tmem_ld_wait(o);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
-                        tmem_st32(o_at + c * 32, o);
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
+                            tmem_st32(o_at + c * 32, o);
+                        }
                     }
                 }
-            }
-            const float2 scale2 = make_float2(p.sl2, p.sl2), ref2 = make_float2(-ref, -ref);
+                const float2 scale2 = make_float2(p.sl2, p.sl2), ref2 = make_float2(-ref, -ref);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t w[32];
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t w[32];
 #pragma unroll
-                for (int e = 0; e < 64; e += 2) {
-                    const float2 y = fma2(make_float2(__uint_as_float(x[2 * h + e / 32][e % 32]), __uint_as_float(x[2 * h + e / 32][e % 32 + 1])),
-                                          scale2, ref2);
-                    const float2 z = make_float2(fast_exp2(y.x), fast_exp2(y.y));
-                    sum = add2(sum, z);
-                    w[e / 2] = pack_bf16(z.x, z.y);
+                    for (int e = 0; e < 64; e += 2) {
+                        const float2 y = fma2(make_float2(__uint_as_float(x[2 * h + e / 32][e % 32]), __uint_as_float(x[2 * h + e / 32][e % 32 + 1])),
+                                              scale2, ref2);
+                        const float2 z = make_float2(fast_exp2(y.x), fast_exp2(y.y));
+                        sum = add2(sum, z);
+                        w[e / 2] = pack_bf16(z.x, z.y);
+                    }
+                    tmem_st32(s_at + h * 32, w);
                 }
-                tmem_st32(s_at + h * 32, w);
+                tmem_st_wait();
+                tc_fence_before();
+                mbar_arrive(p_full + 8 * i);
             }
-            tmem_st_wait();
-            tc_fence_before();
-            mbar_arrive(p_full + 8 * i);
-        }
-        float o_scale = 0.f;
-        if (ok && n > 0) {
-            ok = mbar_wait(o_done + 8 * i, (n - 1) & 1, &s_abort, status, 7);
-            ok = __all_sync(0xffffffffu, ok);
-            tc_fence_after();
-            const float l = sum.x + sum.y;
-            o_scale = l == 0.f ? 0.f : 1.f / l;
-        }
-        if (ok) {
-            char *to = p.out + (int64_t)(q0 + token) * p.out_token + (int64_t)(group * p.G + row % p.G) * p.out_head;
+            float o_scale = 0.f;
+            if (ok && n > 0) {
+                ok = mbar_wait(o_done + 8 * i, done + n - 1 & 1, &s_abort, status, 7);
+                ok = __all_sync(0xffffffffu, ok);
+                tc_fence_after();
+                const float l = sum.x + sum.y;
+                o_scale = l == 0.f ? 0.f : 1.f / l;
+            }
+            done += n;
+            if (ok) {
+                char *to = p.out + (int64_t)(u.q0 + token) * p.out_token + (int64_t)(u.group * p.G + row_head) * p.out_head;
 #pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
-                uint32_t o[32];
-                if (n > 0) {
-                    tmem_ld32_issue(o_at + c * 32, o);
-                    tmem_ld_wait(o);
-                }
-                if (used) {
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t o[32];
+                    if (n > 0) {
+                        tmem_ld32_issue(o_at + c * 32, o);
+                        tmem_ld_wait(o);
+                    }
+                    if (used) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        uint32_t w[4];
+                        for (int e = 0; e < 4; ++e) {
+                            uint32_t w[4];
 #pragma unroll
-                        for (int b = 0; b < 4; ++b)
-                            w[b] = n > 0 && limit > 0 ? pack_bf16(__uint_as_float(o[8 * e + 2 * b]) * o_scale, __uint_as_float(o[8 * e + 2 * b + 1]) * o_scale) : 0;
-                        *reinterpret_cast<uint4 *>(to + c * 64 + e * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+                            for (int b = 0; b < 4; ++b)
+                                w[b] = n > 0 && limit > 0 ? pack_bf16(__uint_as_float(o[8 * e + 2 * b]) * o_scale, __uint_as_float(o[8 * e + 2 * b + 1]) * o_scale) : 0;
+                            *reinterpret_cast<uint4 *>(to + c * 64 + e * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
                     }
                 }
             }
