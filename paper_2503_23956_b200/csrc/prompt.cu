@@ -18,7 +18,8 @@
 // tensor core has the other tile's products.  MMAs of one thread are executed in order, so S_i of the next key tile is issued right behind
 // the product that reads P_i.
 //
-// The reference of a row moves only when a logit is more than 2^8 above it; then its warp rescales O_i in tensor
+// The reference of a row moves only when a logit is more than 2^16 above it (weights are floating-point numbers: it
+// need not be the maximum); then its warp rescales O_i in tensor
 // memory, behind the last product's commit.  Sums and O_i in fp32.  P is rounded to bf16 (2^-9 of a weight, averaged over
 // the keys, beside 2^-9 of the rounding of the output).
 //
@@ -38,6 +39,7 @@ namespace {
 __device__ uint32_t g_prompt_status;   // set when a bounded wait gave up
 
 constexpr int kKeys = 128;             // keys of a tile
+constexpr float kRise = 16.f;          // a row's reference moves when a logit is more than this above it (log2)
 
 struct PromptParams {
     const int32_t *q_offsets, *k_offsets;
@@ -57,33 +59,56 @@ struct PromptCfg {
     static constexpr int THREADS = 384;                  // three warpgroups of 168 registers a thread, moved below
 };
 
-// PV: bf16 x bf16 -> fp32, A from tensor memory (K-major), B from shared memory with N contiguous
-__device__ __forceinline__ void umma_bf16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+// Matrix descriptors (umma_desc_sw128) as their two words: the upper one is the same for every tile here (groups of 8 rows
+// 1024 bytes apart, version, 128-byte swizzle), the lower one is the start address in units of 16 bytes and, for a tile whose
+// rows are the K axis (V), the distance to the next 64 elements of N.  One thread issues some 24 products in a thousand
+// cycles: with the whole descriptor built for each of them that took it 2500.
+constexpr uint32_t kDescHigh = (1024 >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t desc_low(uint32_t smem_addr) { return smem_addr >> 4 | 1u << 16; }
+__device__ __forceinline__ uint32_t desc_low_rows_are_k(uint32_t smem_addr) { return smem_addr >> 4 | (uint32_t)(kKeys * 128 >> 4) << 16; }
+
+// D[tmem] (+)= A[smem] B[smem]^T, bf16, one step of 16 of the K axis
+__device__ __forceinline__ void mma_smem(uint32_t tmem_d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate) {
     asm volatile(
-        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
-        ::"r"(tmem_d), "r"(tmem_a), "l"(b_desc), "r"(idesc), "r"(accumulate)
-        : "memory");
+        "{\n.reg .pred p;\n.reg .b64 a, b;\nmov.b64 a, {%1, %4};\nmov.b64 b, {%2, %4};\nsetp.ne.b32 p, %5, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}\n"
+        ::"r"(tmem_d), "r"(a), "r"(b), "r"(idesc), "r"(kDescHigh), "r"((uint32_t)accumulate) : "memory");
 }
-// 128-byte swizzled tile whose rows are the K axis (keys) and whose 128 bytes are 64 elements of N: groups of 8 rows are
-// 1024 bytes apart, the next 64 elements of N kKeys rows.
-__device__ __forceinline__ uint64_t umma_desc_rows_are_k(uint32_t smem_addr) {
-    uint64_t d = umma_desc_sw128(smem_addr) & ~((uint64_t)0x3fff << 16);
-    return d | (uint64_t)((kKeys * 128) >> 4) << 16;
-}
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+// the same with A in tensor memory
+__device__ __forceinline__ void mma_tmem(uint32_t tmem_d, uint32_t tmem_a, uint32_t b, uint32_t idesc, bool accumulate) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
-          "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
-          "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-        : "memory");
+        "{\n.reg .pred p;\n.reg .b64 b;\nmov.b64 b, {%2, %4};\nsetp.ne.b32 p, %5, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}\n"
+        ::"r"(tmem_d), "r"(tmem_a), "r"(b), "r"(idesc), "r"(kDescHigh), "r"((uint32_t)accumulate) : "memory");
 }
+// 16 columns of this thread's lane as they are
+#define AIRCACHE_R16(c, r) c(r[0]), c(r[1]), c(r[2]), c(r[3]), c(r[4]), c(r[5]), c(r[6]), c(r[7]), \
+    c(r[8]), c(r[9]), c(r[10]), c(r[11]), c(r[12]), c(r[13]), c(r[14]), c(r[15])
+__device__ __forceinline__ void tmem_st16_bits(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(taddr), AIRCACHE_R16("r", r) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16_bits(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : AIRCACHE_R16("=r", r) : "r"(taddr) : "memory");
+}
+#undef AIRCACHE_R16
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
+}
+
+// 16 columns of tensor memory times `shrink`.
+__device__ __forceinline__ void rescale16(uint32_t at, float shrink) {
+    uint32_t r[16];
+    tmem_ld16_bits(at, r);
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        r[e] = __float_as_uint(__uint_as_float(r[e]) * shrink);
+    tmem_st16_bits(at, r);
+    tmem_st_wait();
 }
 
 // Asks for a block of this grid that has not started yet; the answer (16 bytes) is counted on an mbarrier.
@@ -159,7 +184,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     __syncthreads();
     tc_fence_after();
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const uint32_t tmem = s_tmem;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
     // The unit of turn `it`, as the producer has left it.
     auto next_unit = [&](int it, Unit &u) {
         const bool ok = __all_sync(0xffffffffu, mbar_wait(unit_full + 8 * (it & 1), it >> 1 & 1, &s_abort, status, 8));
@@ -259,81 +284,88 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         } else if (warp == 9) {
             const uint32_t idesc_s = umma_idesc_bf16(128, kKeys);
             const uint32_t idesc_o = umma_idesc_bf16(128, D) | 1u << 16;   // B with N contiguous
+            constexpr uint32_t kTileLow = C::TILE >> 4, kHalfLow = C::HALF >> 4;   // in units of 16 bytes
+            const uint32_t q_low = desc_low(q_smem), k_low = desc_low(ring), v_low = desc_low_rows_are_k(ring);
             bool ok = true;
-            int base = 0, seen = 0, full_units = 0;   // tiles of the ring: in front of this unit, waited for
-            int done[2] = {0, 0};                     // key tiles of either row tile in front of this unit
+            int k_slot = 0, v_slot = 1, k_round = 0, v_round = 0, full_units = 0;   // ring slots of the next K and V tile, how often each went round
+            int done[2] = {0, 0};                                                  // key tiles of either row tile in front of this unit
             Unit u;
             for (int it = 0; ok && next_unit(it, u); ++it) {
-                const int n_tiles = max(u.tiles[0], u.tiles[1]);
-                if (n_tiles == 0) continue;
-                auto arrived = [&](int c) {
-                    for (; ok && seen <= base + c; ++seen)
-                        ok = __all_sync(0xffffffffu, mbar_wait(kv_full + 8 * (seen % C::SLOTS), seen / C::SLOTS & 1, &s_abort, status, 3));
+                // (every lane has the same; said so that the compiler can keep addresses in uniform registers)
+                const int n_k = __shfl_sync(0xffffffffu, u.n_k, 0);
+                const int tiles[2] = {__shfl_sync(0xffffffffu, u.tiles[0], 0), __shfl_sync(0xffffffffu, u.tiles[1], 0)};
+                const int n = max(tiles[0], tiles[1]);
+                if (n == 0) continue;
+                auto wait_for = [&](uint32_t bar, int parity, uint32_t code) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, &s_abort, status, code));
                     tc_fence_after();
                 };
-                auto scores = [&](int i, int j) {   // S_i = Q_i K_j^T
-                    if (elect_one()) {
-                        const uint32_t k_tile = ring + ((base + 2 * j) % C::SLOTS) * C::TILE;
+                auto scores = [&](int i) {   // S_i = Q_i K^T with the K tile at k_slot
+                    const uint32_t a = q_low + i * kTileLow, b = k_low + k_slot * kTileLow;
 #pragma unroll
-                        for (int s = 0; s < D / 16; ++s)
-                            umma_bf16(tmem + i * kKeys, umma_desc_sw128(q_smem + i * C::TILE + (s >> 2) * C::HALF + (s & 3) * 32),
-                                      umma_desc_sw128(k_tile + (s >> 2) * C::HALF + (s & 3) * 32), idesc_s, s > 0);
-                        umma_commit(s_full + 8 * i);
-                    }
-                    __syncwarp();
+                    for (int s = 0; s < D / 16; ++s)
+                        mma_smem(tmem + i * kKeys, a + (s >> 2) * kHalfLow + (s & 3) * 2, b + (s >> 2) * kHalfLow + (s & 3) * 2, idesc_s, s > 0);
+                    umma_commit(s_full + 8 * i);
                 };
-                auto commit = [&](uint32_t bar) {
-                    if (elect_one()) umma_commit(bar);
-                    __syncwarp();
+                auto next_tile = [&](int &slot, int &round) {
+                    slot += 2;
+                    if (slot >= C::SLOTS) { slot -= C::SLOTS; ++round; }
                 };
-                auto release = [&](int c) { commit(kv_empty + 8 * ((base + c) % C::SLOTS)); };
-                ok = __all_sync(0xffffffffu, mbar_wait(q_full, full_units & 1, &s_abort, status, 2));
+                wait_for(q_full, full_units & 1, 2);
                 ++full_units;
-                arrived(0);
+                if (ok) wait_for(kv_full + 8 * k_slot, k_round & 1, 3);
                 if (!ok) break;
-                for (int i = 0; i < 2; ++i)
-                    if (u.tiles[i] > 0) scores(i, 0);
-                release(0);
-                if (n_tiles == 1) commit(q_empty);
-                for (int j = 0; ok && j < n_tiles; ++j) {
-                    const uint32_t v_tile = ring + ((base + 2 * j + 1) % C::SLOTS) * C::TILE;
-                    arrived(2 * j + 1);
+                if (elect_one()) {
+                    if (tiles[0] > 0) scores(0);
+                    if (tiles[1] > 0) scores(1);
+                    umma_commit(kv_empty + 8 * k_slot);
+                    if (n == 1) umma_commit(q_empty);
+                }
+                __syncwarp();
+                next_tile(k_slot, k_round);
+                for (int j = 0; j < n; ++j) {
+                    wait_for(kv_full + 8 * v_slot, v_round & 1, 3);
                     if (!ok) break;
-                    const int rows = u.n_k - j * kKeys;
+                    const int rows = n_k - j * kKeys;
                     if (rows < kKeys) {   // keys behind the sequence's last: zeros
                         for (int e = lane; e < (kKeys - rows) * C::HALVES * 8; e += 32) {
-                            const uint32_t at = v_tile + (e / ((kKeys - rows) * 8)) * C::HALF + rows * 128 + e % ((kKeys - rows) * 8) * 16;
+                            const uint32_t at = ring + v_slot * C::TILE + (e / ((kKeys - rows) * 8)) * C::HALF + rows * 128 + e % ((kKeys - rows) * 8) * 16;
                             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
                         }
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
                     }
-                    for (int i = 0; i < 2 && ok; ++i) {
-                        if (j < u.tiles[i]) {
-                            ok = __all_sync(0xffffffffu, mbar_wait(p_full + 8 * i, done[i] + j & 1, &s_abort, status, 4));
-                            if (!ok) break;
-                            tc_fence_after();
-                            if (elect_one()) {
+                    if (j + 1 < n) wait_for(kv_full + 8 * k_slot, k_round & 1, 3);
+                    if (!ok) break;
+                    const uint32_t v = v_low + v_slot * kTileLow;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if (j < tiles[i]) {
+                            if (ok) wait_for(p_full + 8 * i, done[i] + j & 1, 4);
+                            if (ok && elect_one()) {
 #pragma unroll
                                 for (int s = 0; s < kKeys / 16; ++s)
-                                    umma_bf16_ts(tmem + 256 + i * 128, tmem + i * kKeys + s * 8, umma_desc_rows_are_k(v_tile + s * 2048),
-                                                 idesc_o, j > 0 || s > 0);
+                                    mma_tmem(tmem + 256 + i * 128, tmem + i * kKeys + s * 8, v + s * (2048 >> 4), idesc_o, j > 0 || s > 0);
                                 umma_commit(o_done + 8 * i);
+                                if (i == 1) umma_commit(kv_empty + 8 * v_slot);
+                                if (j + 1 < tiles[i]) scores(i);   // over the columns that the product just issued reads
                             }
-                            __syncwarp();
+                        } else if (i == 1 && elect_one()) {
+                            umma_commit(kv_empty + 8 * v_slot);
                         }
-                        if (i == 1) release(2 * j + 1);
-                        if (j + 1 < u.tiles[i]) {
-                            arrived(2 * j + 2);
-                            if (ok) scores(i, j + 1);
-                        }
+                        __syncwarp();
                     }
-                    if (ok && j + 1 < n_tiles) release(2 * j + 2);
-                    if (ok && j + 2 == n_tiles) commit(q_empty);   // (the unit's last scores are issued)
+                    if (!ok) break;
+                    if (j + 1 < n && elect_one()) {
+                        umma_commit(kv_empty + 8 * k_slot);
+                        if (j + 2 == n) umma_commit(q_empty);   // (the unit's last scores are issued)
+                    }
+                    __syncwarp();
+                    next_tile(v_slot, v_round);
+                    if (j + 1 < n) next_tile(k_slot, k_round);
                 }
-                base += 2 * n_tiles;
-                done[0] += u.tiles[0];
-                done[1] += u.tiles[1];
+                done[0] += tiles[0];
+                done[1] += tiles[1];
             }
         }
     } else {
@@ -376,7 +408,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     for (int e = 0; e < 32; e += 2)
                         top[c] = fmaxf(top[c], fmaxf(__uint_as_float(x[c][e]), __uint_as_float(x[c][e + 1])));
                 const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.sl2;
-                const bool moves = now > ref + 8.f;
+                const bool moves = now > ref + kRise;
                 if (__any_sync(0xffffffffu, moves)) {
                     const float to = moves ? now : ref, shrink = fast_exp2(ref - to);
                     ref = to;
@@ -387,29 +419,21 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                         tc_fence_after();
 #pragma unroll 1
-                        for (int c = 0; c < D / 32; ++c) {
-                            uint32_t o[32];
-                            tmem_ld32_issue(o_at + c * 32, o);
-                            tmem_ld_wait(o);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
-                            tmem_st32(o_at + c * 32, o);
-                        }
+                        for (int b = 0; b < D / 16; ++b) rescale16(o_at + b * 16, shrink);
                     }
                 }
                 const float2 scale2 = make_float2(p.sl2, p.sl2), ref2 = make_float2(-ref, -ref);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t w[32];
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t w[16];
 #pragma unroll
-                    for (int e = 0; e < 64; e += 2) {
-                        const float2 y = fma2(make_float2(__uint_as_float(x[2 * h + e / 32][e % 32]), __uint_as_float(x[2 * h + e / 32][e % 32 + 1])),
-                                              scale2, ref2);
+                    for (int e = 0; e < 32; e += 2) {
+                        const float2 y = fma2(make_float2(__uint_as_float(x[c][e]), __uint_as_float(x[c][e + 1])), scale2, ref2);
                         const float2 z = make_float2(fast_exp2(y.x), fast_exp2(y.y));
                         sum = add2(sum, z);
                         w[e / 2] = pack_bf16(z.x, z.y);
                     }
-                    tmem_st32(s_at + h * 32, w);
+                    tmem_st16_bits(s_at + c * 16, w);
                 }
                 tmem_st_wait();
                 tc_fence_before();
