@@ -196,7 +196,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     };
 
     if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (warp == 8) {
             int block = blockIdx.x, slot = 0, loaded = 0, full_units = 0;
             bool ok = true;
@@ -369,7 +369,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             }
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int i = warp >> 2, row = tid & 127;
         const int row_token = row / p.G, row_head = row - row_token * p.G;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;          // 32 * (warp % 4) tensor-memory lanes
