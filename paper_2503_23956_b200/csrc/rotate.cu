@@ -1,11 +1,16 @@
 // aircache_rotate: norms of queries and keys for each head, rotary positions and the store into the cache, one pass.
 //
 // For a head x (of a token at position pos):  y = x * rsqrt(mean(x^2) + eps) * w,  then every pair (a, b) of frequency i
-// turns by pos * f_i:  (y_a c - y_b s, y_b c + y_a s).  2 bytes in and 2 bytes out per channel and some 10 operations: bound
-// by memory.  A lane holds 8 channels (16 bytes), a head is 16 (8) lanes, so a warp takes two (four) heads of a token
-// at a time, kBatch such loads under way at once; the pair of channels i and i + R/2 is a shuffle apart.  Heads of one token
-// go to one warp where there are many tokens: cosines and sines, eight per lane, are then taken once for all of
-// them.  Where there are few, they go to more warps.
+// turns by pos * f_i:  (y_a c - y_b s, y_b c + y_a s).  2 bytes in and 2 bytes out per channel: bound by memory, once the
+// arithmetic is kept small.  A head is 16 (8) lanes, so a warp takes two (four) heads of a token at a time, kBatch such loads
+// under way at once.  A lane holds both channels of its four pairs (8 bytes from either half of the rotated channels, or 16
+// consecutive bytes in the interleaved layout): no exchange between lanes but for the norm's sum, and four cosines and
+// sines a token.  (With 16 consecutive bytes per lane in both layouts, partners fetched by shuffles: 174 us for 27136
+// tokens of 28 + 2 * 4 heads.)  Heads of one token go to one warp where there are many tokens: the angles are
+// then taken once for all of them.  Where there are few, they go to more warps.  27136 tokens, us: 117 with four loads under
+// way and 20 warps an SM, 103 with two and 32 (4.8 TB/s; the norm's sum takes 13 of it, the angles 4).  Measured and not kept: the next
+// loads asked for ahead of the angles and of a batch's arithmetic (107), two numbers an instruction (105 to 109), the
+// sums of a batch side by side (109), one load under way and 40 warps (118).
 //
 // Angles: pos * f_i in fp32 is off by up to 2^-24 * pos radians, 0.03 at half a million.  The product is exact in fp64
 // (31 + 24 bits), taken in turns and reduced to [-1/2, 1/2] there; sincospif does the rest.
@@ -16,7 +21,7 @@ namespace aircache {
 
 namespace {
 
-constexpr int kBatch = 4;
+constexpr int kBatch = 2;
 
 struct RotateParams {
     const char *q, *k, *v;
@@ -33,7 +38,6 @@ struct RotateParams {
     float eps, factor;
 };
 
-__device__ __forceinline__ float2 bf16x2_f32(uint32_t w) { return make_float2(bf16lo(w), bf16hi(w)); }
 __device__ __forceinline__ uint32_t f32_bf16x2(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -41,12 +45,13 @@ __device__ __forceinline__ uint32_t f32_bf16x2(float lo, float hi) {
 }
 
 template <int D, bool INTERLEAVED>
-__global__ void __launch_bounds__(128) rotate_kernel(RotateParams p) {
+__global__ void __launch_bounds__(128, 8) rotate_kernel(RotateParams p) {
     constexpr int LPH = D / 8;         // lanes of a head
     constexpr int HPW = 32 / LPH;      // heads a warp takes at a time
     const int lane = threadIdx.x & 31, l = lane % LPH, sub = lane / LPH;
-    const int c0 = 8 * l;
-    const bool turns = c0 < 2 * p.half;
+    // the lane's channels: lo .. lo + 3 and hi .. hi + 3, channel lo + e turns with hi + e (interleaved: with its neighbour)
+    const bool turns = 4 * l < p.half;
+    const int lo = turns && !INTERLEAVED ? 4 * l : 8 * l, hi = turns && !INTERLEAVED ? p.half + 4 * l : lo + 4;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5); item < p.items; item += (int64_t)gridDim.x * 4) {
@@ -54,104 +59,88 @@ __global__ void __launch_bounds__(128) rotate_kernel(RotateParams p) {
         const int64_t lt = item / p.parts;
         const int t = (int)(lt % p.n_tokens);
         const int64_t layer = lt / p.n_tokens;
-        int64_t row = p.rows ? p.rows[t] : t;
+        const int64_t row = p.rows ? p.rows[t] : t;
         const bool stored = row >= 0 && row < p.n_rows;
-        float c[8], s[8];
+        const int first = part * p.slots_per_part, last = min(p.slots, first + p.slots_per_part);
+        float c[4], s[4];   // of pairs 4 l .. 4 l + 3
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (INTERLEAVED && (e & 1)) { c[e] = c[e - 1]; s[e] = s[e - 1]; continue; }
+        for (int e = 0; e < 4; ++e) {
             c[e] = 1.f;
             s[e] = 0.f;
             if (turns) {
-                const int i = INTERLEAVED ? (c0 + e) / 2 : (c0 < p.half ? c0 : c0 - p.half) + e;
+                const int i = 4 * l + e;
                 const int axis = i < p.sec0 ? 0 : (i < p.sec01 ? 1 : 2);
                 const double angle = (double)p.positions[(int64_t)axis * p.n_tokens + t] * (double)p.inv_freq[i];
                 const double turn = angle * 0.15915494309189535;   // 1 / (2 pi)
                 sincospif(2.f * (float)(turn - rint(turn)), &s[e], &c[e]);
                 c[e] *= p.factor;
                 s[e] *= p.factor;
-                if (!INTERLEAVED && c0 < p.half) s[e] = -s[e];   // of the first channel of a pair
             }
         }
-        uint4 wq = make_uint4(0, 0, 0, 0), wk = wq;
-        if (p.q_weight) wq = *reinterpret_cast<const uint4 *>(p.q_weight + layer * D + c0);
-        if (p.k_weight) wk = *reinterpret_cast<const uint4 *>(p.k_weight + layer * D + c0);
-        int partner = lane;
-        if (!INTERLEAVED && turns) partner = lane + (c0 < p.half ? p.half / 8 : -(p.half / 8));
-
-        const int first = part * p.slots_per_part;
-        const int last = min(p.slots, first + p.slots_per_part);
-        for (int base = first; base < last; base += HPW * kBatch) {
-            uint4 x[kBatch];
-#pragma unroll
-            for (int b = 0; b < kBatch; ++b) {
-                const int h = base + b * HPW + sub;
-                x[b] = make_uint4(0, 0, 0, 0);
-                if (h < last) {
-                    const char *src = h < p.Hq ? p.q + layer * p.q_l + t * p.q_t + h * p.q_h
-                                    : h < p.Hq + p.Hkv ? p.k + layer * p.k_l + t * p.k_t + (h - p.Hq) * p.k_h
-                                                       : p.v + layer * p.v_l + t * p.v_t + (h - p.Hq - p.Hkv) * p.v_h;
-                    x[b] = *reinterpret_cast<const uint4 *>(src + 2 * c0);
-                }
+        // heads [from, to) of the queries or keys
+        auto rotate_heads = [&](const char *src, int64_t src_head, char *dst, int64_t dst_head, const uint16_t *weight, int from, int to) {
+            float w[8];
+            if (weight) {
+                const uint2 a = *reinterpret_cast<const uint2 *>(weight + layer * D + lo), b = *reinterpret_cast<const uint2 *>(weight + layer * D + hi);
+                w[0] = bf16lo(a.x); w[1] = bf16hi(a.x); w[2] = bf16lo(a.y); w[3] = bf16hi(a.y);
+                w[4] = bf16lo(b.x); w[5] = bf16hi(b.x); w[6] = bf16lo(b.y); w[7] = bf16hi(b.y);
             }
+            src += (from + sub) * src_head;
+            dst += (from + sub) * dst_head;
+            const int64_t src_step = HPW * src_head, dst_step = HPW * dst_head;
+            for (int base = from; base < to; base += HPW * kBatch) {
+                uint2 x[kBatch][2];
 #pragma unroll
-            for (int b = 0; b < kBatch; ++b) {
-                if (base + b * HPW >= last) break;   // (of the whole warp)
-                const int h = base + b * HPW + sub;
-                const bool is_v = h >= p.Hq + p.Hkv;
-                float y[8];
-                const uint32_t xw[4] = {x[b].x, x[b].y, x[b].z, x[b].w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 f = bf16x2_f32(xw[i]);
-                    y[2 * i] = f.x;
-                    y[2 * i + 1] = f.y;
+                for (int b = 0; b < kBatch; ++b) {
+                    x[b][0] = x[b][1] = make_uint2(0, 0);
+                    if (base + b * HPW + sub < to) {
+                        x[b][0] = *reinterpret_cast<const uint2 *>(src + 2 * lo);
+                        x[b][1] = *reinterpret_cast<const uint2 *>(src + 2 * hi);
+                    }
+                    src += src_step;
                 }
-                const uint16_t *weight = h < p.Hq ? p.q_weight : p.k_weight;
-                if (p.q_weight || p.k_weight) {
-                    float sum = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) sum = fmaf(y[i], y[i], sum);
+                for (int b = 0; b < kBatch; ++b) {
+                    if (base + b * HPW >= to) break;   // (of the whole warp)
+                    float y[8] = {bf16lo(x[b][0].x), bf16hi(x[b][0].x), bf16lo(x[b][0].y), bf16hi(x[b][0].y),
+                                  bf16lo(x[b][1].x), bf16hi(x[b][1].x), bf16lo(x[b][1].y), bf16hi(x[b][1].y)};
+                    if (weight) {
+                        float sum = 0.f;
 #pragma unroll
-                    for (int o = 1; o < LPH; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                    if (weight && !is_v) {
+                        for (int e = 0; e < 8; ++e) sum = fmaf(y[e], y[e], sum);
+#pragma unroll
+                        for (int o = 1; o < LPH; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
                         const float r = rsqrtf(sum * (1.f / D) + p.eps);
-                        const uint4 w = h < p.Hq ? wq : wk;
-                        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float2 f = bf16x2_f32(ww[i]);
-                            y[2 * i] *= r * f.x;
-                            y[2 * i + 1] *= r * f.y;
+                        for (int e = 0; e < 8; ++e) y[e] *= r * w[e];
+                    }
+                    if (turns) {   // (channels that do not turn keep their value: 1 * y + 0 * y would make NaN of an infinity)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float &a = y[INTERLEAVED ? 2 * e : e], &b2 = y[INTERLEAVED ? 2 * e + 1 : 4 + e];
+                            const float turned = a * c[e] - b2 * s[e];
+                            b2 = b2 * c[e] + a * s[e];
+                            a = turned;
                         }
                     }
-                }
-                float o[8];
-#pragma unroll
-                for (int i = 0; i < 8; i += 2) {
-                    if (INTERLEAVED) {
-                        o[i] = y[i] * c[i] - y[i + 1] * s[i];
-                        o[i + 1] = y[i + 1] * c[i] + y[i] * s[i];
-                    } else {
-                        o[i] = y[i] * c[i] + __shfl_sync(0xffffffffu, y[i], partner) * s[i];
-                        o[i + 1] = y[i + 1] * c[i + 1] + __shfl_sync(0xffffffffu, y[i + 1], partner) * s[i + 1];
+                    if (base + b * HPW + sub < to) {
+                        *reinterpret_cast<uint2 *>(dst + 2 * lo) = make_uint2(f32_bf16x2(y[0], y[1]), f32_bf16x2(y[2], y[3]));
+                        *reinterpret_cast<uint2 *>(dst + 2 * hi) = make_uint2(f32_bf16x2(y[4], y[5]), f32_bf16x2(y[6], y[7]));
                     }
-                }
-                uint4 out;
-                // (channels that do not turn keep their bits where there is no norm: 1 * y + y * 0 would make NaN of an infinity)
-                const float *z = turns ? o : y;
-                out.x = f32_bf16x2(z[0], z[1]);
-                out.y = f32_bf16x2(z[2], z[3]);
-                out.z = f32_bf16x2(z[4], z[5]);
-                out.w = f32_bf16x2(z[6], z[7]);
-                if (is_v) out = x[b];
-                if (h < last && (h < p.Hq || stored)) {
-                    char *dst = h < p.Hq ? p.q_out + layer * p.qo_l + t * p.qo_t + h * p.qo_h
-                              : !is_v ? p.k_out + layer * p.ko_l + row * p.ko_t + (h - p.Hq) * p.ko_h
-                                      : p.v_out + layer * p.vo_l + row * p.vo_t + (h - p.Hq - p.Hkv) * p.vo_h;
-                    *reinterpret_cast<uint4 *>(dst + 2 * c0) = out;
+                    dst += dst_step;
                 }
             }
+        };
+        if (first < p.Hq)
+            rotate_heads(p.q + layer * p.q_l + t * p.q_t, p.q_h, p.q_out + layer * p.qo_l + t * p.qo_t, p.qo_h, p.q_weight, first,
+                         min(last, p.Hq));
+        if (last > p.Hq && stored) {
+            if (first < p.Hq + p.Hkv)
+                rotate_heads(p.k + layer * p.k_l + t * p.k_t, p.k_h, p.k_out + layer * p.ko_l + row * p.ko_t, p.ko_h, p.k_weight,
+                             max(first - p.Hq, 0), min(last - p.Hq, p.Hkv));
+            for (int h = max(first - p.Hq - p.Hkv, 0) + sub; h < last - p.Hq - p.Hkv; h += HPW)
+                *reinterpret_cast<uint4 *>(p.v_out + layer * p.vo_l + row * p.vo_t + h * p.vo_h + 16 * l) =
+                    *reinterpret_cast<const uint4 *>(p.v + layer * p.v_l + t * p.v_t + h * p.v_h + 16 * l);
         }
     }
 }
