@@ -128,7 +128,7 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     int *s_off = s_P + kMaxRegions + 1, *s_len = s_off + kMaxRegions;
     __shared__ float4 s_state[C::WARPS * 4];   // references and sums of a warp's heads
     __shared__ int s_sum[C::WARPS], s_free[C::WARPS];
-    __shared__ int s_last;
+    __shared__ int s_last[2];   // items to be merged by this CTA: its last one, its first one
     __shared__ volatile int s_abort;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -142,6 +142,7 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     }
     if (tid == 0) {
         s_abort = 0;
+        s_last[0] = s_last[1] = -1;
         asm volatile("prefetch.tensormap [%0];\nprefetch.tensormap [%1];" ::"l"(&tm_k), "l"(&tm_v) : "memory");
     }
     {   // asked into L2 ahead of the wait (no value is used): lengths, first rows, this block's share of the queries
@@ -157,7 +158,7 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     // The CTA's tiles [t0, t1) and, of the item that they begin in: its number, first tile, end, first row, rows.
     const int cta = blockIdx.x;
     const bool pieces = p.items <= (int)gridDim.x;
-    int t0, t1, item, item_first, item_end, item_off, n, c_first = 0, c_last = 0, total = 0, ctas = gridDim.x;
+    int t0, t1, item, item_first, item_end, item_off, n, c_first = 0, c_last = 0, lead_first = 0, lead_last = 0, total = 0, ctas = gridDim.x;
     if (pieces) {
         constexpr int RPL = (kMaxDecodeCtas + 31) / 32;
         const int regions = p.items / p.split, rpl = (regions + 31) / 32;
@@ -229,37 +230,35 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
             return;
         }
     } else {
-        // first tile, first row and rows of every item
-        constexpr int PER = (kMaxRegions + C::THREADS) / C::THREADS;   // of kMaxRegions + 1 entries
-        int u[PER], sum = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int at = tid * PER + i;
-            u[i] = 0;
+        // first tile, first row and rows of every item, THREADS of them at a time
+        int base = 0;
+        for (int at0 = 0; at0 < p.items; at0 += C::THREADS) {
+            const int at = at0 + tid;
+            int u = 0;
             if (at < p.items) {
                 const int len = rows_in_use(p.offsets, p.lens, at, p.rows, p.first_region, p.scale_blocks);
                 s_off[at] = (int)p.offsets[at];
                 s_len[at] = len;
-                u[i] = (len + kTile - 1) / kTile;
+                u = (len + kTile - 1) / kTile;
             }
-            sum += u[i];
-        }
-        int incl = sum;
+            int incl = u;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int x = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += x;
-        }
-        if (lane == 31) s_sum[warp] = incl;
-        __syncthreads();
-        int before = incl - sum;
-        for (int w = 0; w < warp; ++w) before += s_sum[w];
+            for (int o = 1; o < 32; o <<= 1) {
+                const int x = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += x;
+            }
+            if (lane == 31) s_sum[warp] = incl;
+            __syncthreads();
+            int before = base + incl - u;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int at = tid * PER + i;
-            if (at <= p.items) s_P[at] = before;
-            before += u[i];
+            for (int w = 0; w < C::WARPS; ++w) {
+                if (w < warp) before += s_sum[w];
+                base += s_sum[w];
+            }
+            if (at < p.items) s_P[at] = before;
+            __syncthreads();
         }
+        if (tid == 0) s_P[p.items] = base;
         __syncthreads();
         total = s_P[p.items];
         for (int i = cta; i < p.items; i += gridDim.x)
@@ -282,7 +281,7 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
     uint32_t parity = 0;
     int ask = tau, ask_stage = 0, ask_item = item, ask_first = item_first, ask_end = item_end, ask_off = item_off, ask_n = n;
     int ask_region = pieces ? item / p.split : item;
-    const int ask_head = pieces && p.split > 1 ? item - ask_region * p.split : head;
+    const int ask_head = p.split > 1 ? item - ask_region * p.split : head;   // (only pieces are of one head)
     // places of the scales of the tiles in the ring, the next one first.  (Places, not values: a move of a value that is being
     // loaded waits for it.)  A tile's scales are loaded while the one before it is worked on.
     int scale_at[C::STAGES];
@@ -376,11 +375,13 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
         }
 
         float acc[NT][C::MT][4], ref[NT][2], sum[NT][2], v_top = 0.f, v_inv = 0.f;
+        bool unset[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int c = 0; c < C::MT; ++c) acc[nt][c][0] = acc[nt][c][1] = acc[nt][c][2] = acc[nt][c][3] = 0.f;
-            ref[nt][0] = ref[nt][1] = -INFINITY;
+            ref[nt][0] = ref[nt][1] = 0.f;   // none yet: the first finite logits set it
+            unset[nt][0] = unset[nt][1] = true;
             sum[nt][0] = sum[nt][1] = 0.f;
         }
 
@@ -400,7 +401,7 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
             if (++stage == C::STAGES) { stage = 0; parity ^= 1; }
 
             const int rows = n - (tau - item_first) * kTile;   // of the tile, kTile or more unless it is the item's last
-            float x[kBlocks][NT][4];
+            float x[kBlocks][NT][4];   // logits (log2) above the reference
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) {
                 float s[NT][2][4];
@@ -428,7 +429,7 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[b][nt][i] = (s[nt][0][i] + s[nt][1][i]) * (f[nt][i & 1] * k_scale);
+                    for (int i = 0; i < 4; ++i) x[b][nt][i] = fmaf(s[nt][0][i] + s[nt][1][i], f[nt][i & 1] * k_scale, -ref[nt][i & 1]);
             }
             if (rows < kTile) {
 #pragma unroll
@@ -448,7 +449,7 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
                     tops[nt][j] = fmaxf(x[0][nt][j], x[0][nt][j + 2]);
 #pragma unroll
                     for (int b = 1; b < kBlocks; ++b) tops[nt][j] = fmaxf(tops[nt][j], fmaxf(x[b][nt][j], x[b][nt][j + 2]));
-                    moves = moves || tops[nt][j] > ref[nt][j] + 4.f;
+                    moves = moves || unset[nt][j] || tops[nt][j] > 4.f;
                 }
             if (__any_sync(0xffffffffu, moves)) {
 #pragma unroll
@@ -459,9 +460,15 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                        const float now = fmaxf(fmaxf(ref[nt][j], top), -1e30f);
-                        const float shrink = fast_exp2(ref[nt][j] - now);
-                        ref[nt][j] = now;
+                        const bool sets = unset[nt][j] && top > -INFINITY;
+                        const float up = sets ? top : unset[nt][j] ? 0.f : fmaxf(top, 0.f), shrink = sets ? 0.f : fast_exp2(-up);
+                        unset[nt][j] = unset[nt][j] && !sets;
+                        ref[nt][j] += up;
+#pragma unroll
+                        for (int b = 0; b < kBlocks; ++b) {
+                            x[b][nt][j] -= up;
+                            x[b][nt][j + 2] -= up;
+                        }
                         sum[nt][j] *= shrink;
 #pragma unroll
                         for (int c = 0; c < C::MT; ++c) {
@@ -489,7 +496,7 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {   // keys g (i = 0) and g + 8
-                        const float p0 = fast_exp2(x[b][nt][2 * i] - ref[nt][0]), p1 = fast_exp2(x[b][nt][2 * i + 1] - ref[nt][1]);
+                        const float p0 = fast_exp2(x[b][nt][2 * i]), p1 = fast_exp2(x[b][nt][2 * i + 1]);
                         sum[nt][0] += p0;
                         sum[nt][1] += p1;
                         const uint32_t hi = f16x2(p0 * vf, p1 * vf);
@@ -544,6 +551,11 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
             do ++next; while (s_P[next + 1] <= item_end);
             load_q(next);
         }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                if (unset[nt][j]) ref[nt][j] = -INFINITY;
         // the end of the item's part: sums over the lanes of a head, true units; then the warps of a head put their states
         // into the ring stages that they have just read and share out the channels of the merged one
         const bool whole = item_first >= t0 && item_end <= t1;
@@ -631,34 +643,20 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
             }
         }
         if (!whole) {
-            __syncthreads();
             if (!pieces) {   // the CTAs that have a part of the item, in order: tile u belongs to CTA ((u + 1) * ctas - 1) / total
                 c_first = (int)(((int64_t)(item_first + 1) * ctas - 1) / total);
                 c_last = (int)(((int64_t)item_end * ctas - 1) / total);
             }
+            __syncthreads();
+            const bool leads = item_end < t1;   // the end of an item that began before this CTA's part
             if (tid == 0) {
                 __threadfence();
-                s_last = atomicAdd(p.tickets + item, 1) == c_last - c_first;
+                s_last[leads] = atomicAdd(p.tickets + item, 1) == c_last - c_first ? item : -1;
                 __threadfence();
             }
-            __syncthreads();
-            if (s_last) {
-                for (int e = tid; e < p.Hq * D; e += C::THREADS) {
-                    const int hq = e / D;
-                    float m = -1e30f, o = 0.f, l = 0.f;
-#pragma unroll 4
-                    for (int c = c_first; c <= c_last; ++c) {
-                        const float *from = p.partials + (2 * (int64_t)c + (c == c_first ? 1 : 0)) * slot_floats;
-                        const float cm = __ldcg(from + (int64_t)p.Hq * D + hq), cl = __ldcg(from + (int64_t)p.Hq * (D + 1) + hq);
-                        const float co = __ldcg(from + e);
-                        const float now = fmaxf(m, cm), mine = fast_exp2(m - now), theirs = fast_exp2(cm - now);
-                        m = now;
-                        l = l * mine + cl * theirs;
-                        o = o * mine + co * theirs;
-                    }
-                    p.out[(int64_t)item * p.Hq * D + e] = l > 0.f || l != l ? o / l : 0.f;
-                }
-                if (tid == 0) p.tickets[item] = 0;
+            if (leads) {   // whether it was the last one is looked at in the end
+                lead_first = c_first;
+                lead_last = c_last;
             }
         }
         if (item_end >= t1) break;
@@ -666,6 +664,36 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
         item_first = item_end;
         item_end = s_P[item + 1];
         n = s_len[item];
+    }
+    // the items whose last part was this CTA's are merged
+    __syncthreads();
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
+        const int item = s_last[which];
+        if (item < 0) continue;
+        const int c0 = which ? lead_first : c_first, c1 = which ? lead_last : c_last;
+        const int64_t slot_floats = partial_slot_floats(p.Hq, D);
+        for (int e = tid; e < p.Hq * D / 4; e += C::THREADS) {   // (four channels a thread: one element each took a trip to L2 after the other)
+            const int hq = e / (D / 4);
+            float m = -1e30f, l = 0.f;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+            for (int c = c0; c <= c1; ++c) {
+                const float *from = p.partials + (2 * (int64_t)c + (c == c0 ? 1 : 0)) * slot_floats;
+                const float cm = __ldcg(from + (int64_t)p.Hq * D + hq), cl = __ldcg(from + (int64_t)p.Hq * (D + 1) + hq);
+                const float4 co = __ldcg(reinterpret_cast<const float4 *>(from) + e);
+                const float now = fmaxf(m, cm), mine = fast_exp2(m - now), theirs = fast_exp2(cm - now);
+                m = now;
+                l = l * mine + cl * theirs;
+                o.x = o.x * mine + co.x * theirs;
+                o.y = o.y * mine + co.y * theirs;
+                o.z = o.z * mine + co.z * theirs;
+                o.w = o.w * mine + co.w * theirs;
+            }
+            const float times = l > 0.f || l != l ? 1.f / l : 0.f;
+            reinterpret_cast<float4 *>(p.out + (int64_t)item * p.Hq * D)[e] = make_float4(o.x * times, o.y * times, o.z * times, o.w * times);
+        }
+        if (tid == 0) p.tickets[item] = 0;
     }
     // a wait that gave up: copies in flight get their time before the block's memory goes
     if (s_abort)
