@@ -49,6 +49,14 @@ struct PromptParams {
     float sl2;
 };
 
+// A block's unit of work: row tiles of one sequence and KV head.
+struct Unit {
+    int q0, n_q, k0, n_k;   // the sequence's rows
+    int first, group;       // first token of the first tile; KV head, -1: no more units
+    int split;              // one row tile, whose key tiles the two halves of the block share: even ones, odd ones
+    int tiles[2];           // key tiles of each half
+};
+
 template <int D>
 struct PromptCfg {
     static constexpr int HALVES = D / 64;
@@ -130,20 +138,14 @@ __device__ __forceinline__ int taken_block(uint32_t answer) {
     return ok ? (int)x : -1;
 }
 
-// A block's unit of work: two row tiles of one sequence and KV head.
-struct Unit {
-    int q0, n_q, k0, n_k;   // the sequence's rows
-    int first, group;       // first token of the first tile; KV head, -1: no more units
-    int tiles[2];           // key tiles of each row tile
-};
-
-template <int D>
+// ROW_TILES = 1: a unit has one row tile, whose key tiles the halves of the block share (split units).
+template <int D, int ROW_TILES>
 __global__ void __launch_bounds__(PromptCfg<D>::THREADS, 1)
 prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
               const __grid_constant__ CUtensorMap tm_v, const PromptParams p) {
     using C = PromptCfg<D>;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ uint64_t s_bars[2 + 2 * C::SLOTS + 6 + 5];
+    __shared__ uint64_t s_bars[2 + 2 * C::SLOTS + 6 + 6];
     __shared__ __align__(16) uint32_t s_answer[4];
     __shared__ Unit s_unit[2];
     __shared__ uint32_t s_tmem;
@@ -153,7 +155,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     const uint32_t bars = smem_u32(s_bars);
     const uint32_t q_full = bars, q_empty = bars + 8, kv_full = bars + 16, kv_empty = kv_full + 8 * C::SLOTS,
                    s_full = kv_empty + 8 * C::SLOTS, p_full = s_full + 16, o_done = p_full + 16, unit_full = o_done + 16,
-                   unit_empty = unit_full + 16, answered = unit_empty + 16;
+                   unit_empty = unit_full + 16, answered = unit_empty + 16, met_all = answered + 8;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int TPT = p.tokens_per_tile;
     uint32_t *status = &g_prompt_status;
@@ -175,6 +177,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             mbar_init(unit_empty + 8 * i, 9);   // a lane of each warp that reads a unit
         }
         mbar_init(answered, 1);
+        mbar_init(met_all, 256);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         s_abort = 0;
         asm volatile("prefetch.tensormap [%0];\nprefetch.tensormap [%1];\nprefetch.tensormap [%2];"
@@ -213,7 +216,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                         if (s < p.n_seqs) {
                             q0 = min(max(p.q_offsets[s], 0), p.q_tokens);
                             n_q = min(max(p.q_offsets[s + 1], q0), p.q_tokens) - q0;
-                            n = (n_q + 2 * TPT - 1) / (2 * TPT);
+                            n = (n_q + ROW_TILES * TPT - 1) / (ROW_TILES * TPT);
                         }
                         int incl = n;
 #pragma unroll
@@ -227,7 +230,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                             const int src = __ffs(who) - 1, at = s0 + src;
                             u.q0 = __shfl_sync(0xffffffffu, q0, src);
                             u.n_q = __shfl_sync(0xffffffffu, n_q, src);
-                            u.first = (unit - __shfl_sync(0xffffffffu, mine, src)) * 2 * TPT;
+                            u.first = (unit - __shfl_sync(0xffffffffu, mine, src)) * ROW_TILES * TPT;
                             u.k0 = min(max(p.k_offsets[at], 0), p.k_tokens);
                             u.n_k = min(max(p.k_offsets[at + 1], u.k0), p.k_tokens) - u.k0;
                         }
@@ -237,7 +240,12 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     for (int i = 0; i < 2; ++i) {   // (a block of a grid larger than the units has no tokens: n_q = 0)
                         const int t0 = u.first + i * TPT, last = min(t0 + TPT, u.n_q) - 1;
                         const int seen = t0 >= u.n_q ? 0 : min(u.n_k, p.causal ? u.n_k - u.n_q + last + 1 : u.n_k);
-                        u.tiles[i] = seen <= 0 ? 0 : (seen + kKeys - 1) / kKeys;
+                        u.tiles[i] = seen <= 0 || i >= ROW_TILES ? 0 : (seen + kKeys - 1) / kKeys;
+                    }
+                    u.split = ROW_TILES == 1 && u.tiles[0] > 1;
+                    if (u.split) {
+                        u.tiles[1] = u.tiles[0] / 2;
+                        u.tiles[0] -= u.tiles[1];
                     }
                 }
                 if (it >= 2) ok = mbar_wait(unit_empty + 8 * (it & 1), (it >> 1) + 1 & 1, &s_abort, status, 9);
@@ -251,11 +259,11 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 if (lane == 0) {
                     mbar_expect_tx(answered, 16);
                     take_block(smem_u32(s_answer), answered);
-                    const int n_tiles = max(u.tiles[0], u.tiles[1]);
+                    const int n_tiles = u.split ? u.tiles[0] + u.tiles[1] : max(u.tiles[0], u.tiles[1]);
                     if (n_tiles > 0) {
                         if (full_units > 0) ok = mbar_wait(q_empty, full_units + 1 & 1, &s_abort, status, 1);
                         if (ok) {
-                            const int n_rows = u.tiles[1] > 0 ? 2 : 1;   // (the second tile has keys whenever it has tokens and the first has)
+                            const int n_rows = u.tiles[1] > 0 && !u.split ? 2 : 1;   // (the second tile has keys whenever it has tokens and the first has)
                             mbar_expect_tx(q_full, n_rows * C::HALVES * 128 * TPT * p.G);
                             for (int i = 0; i < n_rows; ++i)
                                 for (int h = 0; h < C::HALVES; ++h)
@@ -294,14 +302,15 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 // (every lane has the same; said so that the compiler can keep addresses in uniform registers)
                 const int n_k = __shfl_sync(0xffffffffu, u.n_k, 0);
                 const int tiles[2] = {__shfl_sync(0xffffffffu, u.tiles[0], 0), __shfl_sync(0xffffffffu, u.tiles[1], 0)};
+                const bool split = ROW_TILES == 1 && __shfl_sync(0xffffffffu, u.split, 0);
                 const int n = max(tiles[0], tiles[1]);
                 if (n == 0) continue;
                 auto wait_for = [&](uint32_t bar, int parity, uint32_t code) {
                     ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, &s_abort, status, code));
                     tc_fence_after();
                 };
-                auto scores = [&](int i) {   // S_i = Q_i K^T with the K tile at k_slot
-                    const uint32_t a = q_low + i * kTileLow, b = k_low + k_slot * kTileLow;
+                auto scores = [&](int i, uint32_t a) {   // S_i = Q K^T with the Q tile at a and the K tile at k_slot
+                    const uint32_t b = k_low + k_slot * kTileLow;
 #pragma unroll
                     for (int s = 0; s < D / 16; ++s)
                         mma_smem(tmem + i * kKeys, a + (s >> 2) * kHalfLow + (s & 3) * 2, b + (s >> 2) * kHalfLow + (s & 3) * 2, idesc_s, s > 0);
@@ -311,13 +320,66 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     slot += 2;
                     if (slot >= C::SLOTS) { slot -= C::SLOTS; ++round; }
                 };
+                // keys behind the sequence's last in the V tile at v_slot, which has `rows` of it: zeros
+                auto clear_tail = [&](int rows) {
+                    if (rows >= kKeys) return;
+                    for (int e = lane; e < (kKeys - rows) * C::HALVES * 8; e += 32) {
+                        const uint32_t at = ring + v_slot * C::TILE + (e / ((kKeys - rows) * 8)) * C::HALF + rows * 128 + e % ((kKeys - rows) * 8) * 16;
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                };
+                auto product = [&](int i, bool first) {   // O_i (+)= P_i V with the V tile at v_slot
+                    const uint32_t v = v_low + v_slot * kTileLow;
+#pragma unroll
+                    for (int s = 0; s < kKeys / 16; ++s)
+                        mma_tmem(tmem + 256 + i * 128, tmem + i * kKeys + s * 8, v + s * (2048 >> 4), idesc_o, !first || s > 0);
+                    umma_commit(o_done + 8 * i);
+                };
                 wait_for(q_full, full_units & 1, 2);
                 ++full_units;
+                if (split) {   // half i has key tiles i, i + 2, ..: the ring's tiles are for one half each
+                    const int all = tiles[0] + tiles[1];
+                    for (int i = 0; i < 2 && ok; ++i) {
+                        wait_for(kv_full + 8 * k_slot, k_round & 1, 3);
+                        if (ok && elect_one()) {
+                            scores(i, q_low);
+                            umma_commit(kv_empty + 8 * k_slot);
+                            if (i + 1 == all) umma_commit(q_empty);
+                        }
+                        __syncwarp();
+                        next_tile(k_slot, k_round);
+                    }
+                    for (int kt = 0; kt < all && ok; ++kt) {
+                        const int i = kt & 1, j = kt >> 1;
+                        wait_for(kv_full + 8 * v_slot, v_round & 1, 3);
+                        if (ok) clear_tail(n_k - kt * kKeys);
+                        if (ok && kt + 2 < all) wait_for(kv_full + 8 * k_slot, k_round & 1, 3);
+                        if (ok) wait_for(p_full + 8 * i, done[i] + j & 1, 4);
+                        if (ok && elect_one()) {
+                            product(i, j == 0);
+                            umma_commit(kv_empty + 8 * v_slot);
+                            if (kt + 2 < all) {
+                                scores(i, q_low);
+                                umma_commit(kv_empty + 8 * k_slot);
+                                if (kt + 3 == all) umma_commit(q_empty);   // (the unit's last scores are issued)
+                            }
+                        }
+                        __syncwarp();
+                        next_tile(v_slot, v_round);
+                        if (kt + 2 < all) next_tile(k_slot, k_round);
+                    }
+                    if (!ok) break;
+                    done[0] += tiles[0];
+                    done[1] += tiles[1];
+                    continue;
+                }
                 if (ok) wait_for(kv_full + 8 * k_slot, k_round & 1, 3);
                 if (!ok) break;
                 if (elect_one()) {
-                    if (tiles[0] > 0) scores(0);
-                    if (tiles[1] > 0) scores(1);
+                    if (tiles[0] > 0) scores(0, q_low);
+                    if (tiles[1] > 0) scores(1, q_low + kTileLow);
                     umma_commit(kv_empty + 8 * k_slot);
                     if (n == 1) umma_commit(q_empty);
                 }
@@ -326,29 +388,17 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 for (int j = 0; j < n; ++j) {
                     wait_for(kv_full + 8 * v_slot, v_round & 1, 3);
                     if (!ok) break;
-                    const int rows = n_k - j * kKeys;
-                    if (rows < kKeys) {   // keys behind the sequence's last: zeros
-                        for (int e = lane; e < (kKeys - rows) * C::HALVES * 8; e += 32) {
-                            const uint32_t at = ring + v_slot * C::TILE + (e / ((kKeys - rows) * 8)) * C::HALF + rows * 128 + e % ((kKeys - rows) * 8) * 16;
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
-                        }
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                        __syncwarp();
-                    }
+                    clear_tail(n_k - j * kKeys);
                     if (j + 1 < n) wait_for(kv_full + 8 * k_slot, k_round & 1, 3);
                     if (!ok) break;
-                    const uint32_t v = v_low + v_slot * kTileLow;
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         if (j < tiles[i]) {
                             if (ok) wait_for(p_full + 8 * i, done[i] + j & 1, 4);
                             if (ok && elect_one()) {
-#pragma unroll
-                                for (int s = 0; s < kKeys / 16; ++s)
-                                    mma_tmem(tmem + 256 + i * 128, tmem + i * kKeys + s * 8, v + s * (2048 >> 4), idesc_o, j > 0 || s > 0);
-                                umma_commit(o_done + 8 * i);
+                                product(i, j == 0);
                                 if (i == 1) umma_commit(kv_empty + 8 * v_slot);
-                                if (j + 1 < tiles[i]) scores(i);   // over the columns that the product just issued reads
+                                if (j + 1 < tiles[i]) scores(i, q_low + i * kTileLow);   // over the columns that the product just issued reads
                             }
                         } else if (i == 1 && elect_one()) {
                             umma_commit(kv_empty + 8 * v_slot);
@@ -375,12 +425,21 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;          // 32 * (warp % 4) tensor-memory lanes
         const uint32_t s_at = tmem + i * kKeys + lanes, o_at = tmem + 256 + i * 128 + lanes;
         bool ok = true;
-        int done = 0;   // key tiles in front of this unit
+        int done = 0, met = 0;   // key tiles in front of this unit; meetings
+        auto meet = [&]() {      // of both halves; bounded, as every wait
+            tc_fence_before();
+            mbar_arrive(met_all);
+            if (ok) ok = mbar_wait(met_all, met & 1, &s_abort, status, 10);
+            ok = __all_sync(0xffffffffu, ok);
+            ++met;
+            tc_fence_after();
+        };
         Unit u;
         for (int it = 0; ok && next_unit(it, u); ++it) {
-            const int n = u.tiles[i], t0 = u.first + i * TPT, token = t0 + row_token;
-            const bool used = row_token < TPT && token < u.n_q;
+            const int n = u.tiles[i], t0 = u.first + (ROW_TILES == 1 ? 0 : i * TPT), token = t0 + row_token;
+            const bool used = row_token < TPT && token < u.n_q && (ROW_TILES == 2 || i == 0 || u.split);
             const int limit = !used ? 0 : max(0, min(u.n_k, p.causal ? u.n_k - u.n_q + token + 1 : u.n_k));
+            const int kt_step = ROW_TILES == 1 && u.split ? 2 : 1, kt_first = ROW_TILES == 1 && u.split ? i : 0;   // key tiles of this half
             const int all_see = min(u.n_k, p.causal ? u.n_k - u.n_q + t0 + 1 : u.n_k);   // keys that every token of the tile sees
             float ref = -1e30f;
             float2 sum = make_float2(0.f, 0.f);
@@ -393,8 +452,9 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 for (int c = 0; c < 4; ++c) tmem_ld32_issue(s_at + c * 32, x[c]);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld_wait(x[c]);
-                if ((j + 1) * kKeys > all_see) {
-                    const int left = limit - j * kKeys;
+                const int kt = kt_first + j * kt_step;
+                if ((kt + 1) * kKeys > all_see) {
+                    const int left = limit - kt * kKeys;
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -448,6 +508,39 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 o_scale = l == 0.f ? 0.f : 1.f / l;
             }
             done += n;
+            if (ROW_TILES == 1 && u.split) {   // the halves' sums of a row come together; either half writes half of the channels
+                // (references and sums go through the place of the second Q tile, which has none)
+                float2 *const rows = reinterpret_cast<float2 *>(smem_raw + (q_smem - smem_u32(smem_raw)) + C::TILE);
+                rows[i * 128 + row] = make_float2(ref, sum.x + sum.y);
+                meet();
+                const float2 a = rows[row], b = rows[128 + row];
+                const float top = fmaxf(a.x, b.x), wa = fast_exp2(a.x - top), wb = fast_exp2(b.x - top), l = a.y * wa + b.y * wb;
+                const float inv = l == 0.f ? 0.f : 1.f / l, fa = limit > 0 ? wa * inv : 0.f, fb = limit > 0 ? wb * inv : 0.f;
+                char *to = p.out + (int64_t)(u.q0 + token) * p.out_token + (int64_t)(u.group * p.G + row_head) * p.out_head + i * D;
+#pragma unroll 1
+                for (int c = 0; c < D / 64 && ok; ++c) {
+                    uint32_t oa[32], ob[32];
+                    tmem_ld32_issue(tmem + 256 + lanes + i * (D / 2) + c * 32, oa);
+                    tmem_ld32_issue(tmem + 384 + lanes + i * (D / 2) + c * 32, ob);
+                    tmem_ld_wait(oa);
+                    tmem_ld_wait(ob);
+                    if (used) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) {
+                                const int k = 8 * e + 2 * x;
+                                w[x] = limit > 0 ? pack_bf16(fmaf(__uint_as_float(oa[k]), fa, __uint_as_float(ob[k]) * fb),
+                                                             fmaf(__uint_as_float(oa[k + 1]), fa, __uint_as_float(ob[k + 1]) * fb)) : 0;
+                            }
+                            *reinterpret_cast<uint4 *>(to + c * 64 + e * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                    }
+                }
+                meet();   // (the next unit's products go over both halves' sums)
+                continue;
+            }
             if (ok) {
                 char *to = p.out + (int64_t)(u.q0 + token) * p.out_token + (int64_t)(u.group * p.G + row_head) * p.out_head;
 #pragma unroll 1
@@ -495,12 +588,12 @@ int tokens_map(CUtensorMap *tm, const aircache_tokens_t *t, int d, int heads, in
     return rc == CUDA_SUCCESS ? AIRCACHE_OK : AIRCACHE_ERR_UNSUPPORTED;
 }
 
-template <int D>
+template <int D, int ROW_TILES>
 int launch_d(const CUtensorMap &tm_q, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const PromptParams &p, int dev, cudaStream_t st) {
     static std::atomic<uint64_t> allowed[kMaxDevices];
-    const int rc = allow_shared_memory((const void *)prompt_kernel<D>, PromptCfg<D>::SMEM, dev, allowed);
+    const int rc = allow_shared_memory((const void *)prompt_kernel<D, ROW_TILES>, PromptCfg<D>::SMEM, dev, allowed);
     if (rc) return rc;
-    return launch_dependent(prompt_kernel<D>, dim3((unsigned)(p.units * p.n_kv_heads)), dim3(PromptCfg<D>::THREADS), PromptCfg<D>::SMEM, st,
+    return launch_dependent(prompt_kernel<D, ROW_TILES>, dim3((unsigned)(p.units * p.n_kv_heads)), dim3(PromptCfg<D>::THREADS), PromptCfg<D>::SMEM, st,
                             tm_q, tm_k, tm_v, p);
 }
 
@@ -521,19 +614,25 @@ int launch_prompt(const aircache_prompt_t *s, const aircache_tokens_t *q, const 
     p.n_kv_heads = s->n_kv_heads;
     p.G = s->n_q_heads / s->n_kv_heads;
     p.tokens_per_tile = 128 / p.G;
-    p.causal = s->causal;
-    p.sl2 = s->scale * kLog2e;
-    const int64_t units = s->q_tokens / (2 * p.tokens_per_tile) + s->n_seqs;   // at least as many as there are
-    if (units * s->n_kv_heads >= ((int64_t)1 << 31)) return AIRCACHE_ERR_UNSUPPORTED;
-    p.units = (int)units;
     int dev = 0, sms = 0, rc = current_device(&dev, &sms);
     if (rc) return rc;
+    p.causal = s->causal;
+    p.sl2 = s->scale * kLog2e;
+    // One row tile a block, its keys shared by the block's halves, where every block then has an SM of its own: 640 tokens of
+    // a small model 14.0 -> 10.3 us.  In calls of more blocks it reads the keys twice as often (16 turns over some 2000 keys
+    // each, 140 blocks: 51 us with two row tiles, 65 with one).
+    const int row_tiles = ((int64_t)s->q_tokens / p.tokens_per_tile + s->n_seqs) * s->n_kv_heads <= sms ? 1 : 2;
+    const int64_t units = s->q_tokens / (row_tiles * p.tokens_per_tile) + s->n_seqs;   // at least as many as there are
+    if (units * s->n_kv_heads >= ((int64_t)1 << 31)) return AIRCACHE_ERR_UNSUPPORTED;
+    p.units = (int)units;
     CUtensorMap tm_q, tm_k, tm_v;
     if ((rc = tokens_map(&tm_q, q, s->head_dim, s->n_q_heads, s->q_tokens, p.G, p.tokens_per_tile))) return rc;
     const bool keys = s->k_tokens > 0;   // (without keys nothing is loaded)
     if ((rc = tokens_map(&tm_k, keys ? k : q, s->head_dim, keys ? s->n_kv_heads : 1, keys ? s->k_tokens : 1, 1, kKeys))) return rc;
     if ((rc = tokens_map(&tm_v, keys ? v : q, s->head_dim, keys ? s->n_kv_heads : 1, keys ? s->k_tokens : 1, 1, kKeys))) return rc;
-    return s->head_dim == 64 ? launch_d<64>(tm_q, tm_k, tm_v, p, dev, st) : launch_d<128>(tm_q, tm_k, tm_v, p, dev, st);
+    if (row_tiles == 1)
+        return s->head_dim == 64 ? launch_d<64, 1>(tm_q, tm_k, tm_v, p, dev, st) : launch_d<128, 1>(tm_q, tm_k, tm_v, p, dev, st);
+    return s->head_dim == 64 ? launch_d<64, 2>(tm_q, tm_k, tm_v, p, dev, st) : launch_d<128, 2>(tm_q, tm_k, tm_v, p, dev, st);
 }
 
 int prompt_status(cudaStream_t st) {

@@ -116,6 +116,16 @@ def test_which_keys_a_token_sees(Hq, Hkv, d, n_q, n_k, causal):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("Hq,Hkv,d", [(32, 32, 64), (64, 32, 128)])
+@pytest.mark.parametrize("causal", [1, 0])
+def test_calls_of_many_blocks(Hq, Hkv, d, causal):
+    """So many that a block takes two row tiles, not one whose keys its halves share."""
+    n_q, n_k = [700, 1, 129, 300, 257, 640, 33, 128, 450, 90], [700, 900, 129, 500, 257, 640, 33, 60, 450, 1000]
+    check(*inputs(sum(n_q) + 3, sum(n_k), Hq, Hkv, d, seed=6), n_q, n_k, causal)
+    test_which_keys_a_token_sees(Hq, Hkv, d, n_q, n_k, causal)
+
+
+@pytest.mark.gpu
 def test_tokens_that_see_nothing():
     q, k, v = inputs(100, 40, 7, 1, 128)
     out = attend(q, k, v, [100], [40])
