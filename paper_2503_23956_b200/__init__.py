@@ -161,7 +161,7 @@ def _per_token_calls():
         except ImportError:
             _native = False
             return _native
-        if _raw_device is None or _raw_stream is None:
+        if _raw_device is None or _raw_stream is None or not hasattr(_binding, "prompt_attn"):   # (an older build's)
             _native = False
             return _native
         _binding.setup(Shape, Ragged, _raw_device, _raw_stream, Tokens, Rotary, Prompt, Quantized)

@@ -49,7 +49,7 @@ struct DecodeQParams {
     float *partials;     // [2 * CTAs][slot]
     uint32_t *status;
     int64_t rows, scale_blocks, first_region;
-    int items, split;    // split: KV heads per region where an item is a (region, head), else 1
+    int items, n_regions, split;   // split: KV heads per region where an item is a (region, head), else 1
     int row_heads;       // KV heads of a row in memory
     int Hq, G;           // query heads of an item, of a KV head
     float sl2;           // scale * log2(e)
@@ -107,6 +107,16 @@ struct DecodeQCfg {
 
 constexpr int kWholeTiles = 32;   // an item stays whole up to this many tiles (by warps) above the equal share
 
+// a / b for a >= 0, b > 0, through the fp32 divider when both are below 2^23 (an integer division by a run-time divisor costs
+// some hundred cycles of the plan)
+__device__ __forceinline__ int small_div(int a, int b) {
+    if (a >= (1 << 23) || b >= (1 << 23)) return a / b;
+    int q = (int)__fdividef((float)a, (float)b);
+    if (q * b > a) --q;
+    if ((q + 1) * b <= a) ++q;
+    return q;
+}
+
 // largest i with P[i] <= u (P non-decreasing, P[0] = 0, u < P[n])
 __device__ __forceinline__ int find_item(const int *P, int n, int u) {
     int lo = 0, hi = n - 1;
@@ -146,7 +156,7 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
         asm volatile("prefetch.tensormap [%0];\nprefetch.tensormap [%1];" ::"l"(&tm_k), "l"(&tm_v) : "memory");
     }
     {   // asked into L2 ahead of the wait (no value is used): lengths, first rows, this block's share of the queries
-        const int regions = p.items / p.split;
+        const int regions = p.n_regions;
         if (tid * 128 < regions * 4) prefetch_l2(reinterpret_cast<const char *>(p.lens) + tid * 128);
         if (tid * 128 < regions * 8) prefetch_l2(reinterpret_cast<const char *>(p.offsets) + tid * 128);
         const int64_t bytes = (int64_t)p.items * p.Hq * D * 2, at = ((int64_t)tid * gridDim.x + blockIdx.x) * 128;
@@ -157,11 +167,11 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
 
     // The CTA's tiles [t0, t1) and, of the item that they begin in: its number, first tile, end, first row, rows.
     const int cta = blockIdx.x;
-    const bool pieces = p.items <= (int)gridDim.x;
+    constexpr int RPL = 5;   // regions of a lane
+    const bool pieces = p.items <= (int)gridDim.x && p.n_regions <= 32 * RPL;
     int t0, t1, item, item_first, item_end, item_off, n, c_first = 0, c_last = 0, lead_first = 0, lead_last = 0, total = 0, ctas = gridDim.x;
     if (pieces) {
-        constexpr int RPL = (kMaxDecodeCtas + 31) / 32;
-        const int regions = p.items / p.split, rpl = (regions + 31) / 32;
+        const int regions = p.n_regions, rpl = (regions + 31) / 32;
         int len[RPL], off[RPL], un[RPL], sum = 0, most = 0;
 #pragma unroll
         for (int j = 0; j < RPL; ++j) {
@@ -178,47 +188,67 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
         }
         sum = __reduce_add_sync(0xffffffffu, sum) * p.split;
         most = __reduce_max_sync(0xffffffffu, most);
-        const int share = max((sum + ctas - 1) / ctas, 1);
-        int cap = max(most, 1);
-        if (most > share + kWholeTiles / HEADS) {   // the smallest of share, 9/8 of it, ... whose pieces find a CTA each
-            for (cap = share; cap < most; cap += (cap + 7) / 8) {
-                int need = 0;
+        const int share = max(small_div(sum + ctas - 1, ctas), 1);
+        // the CTA's item: of which region (and where that is: its lane and slot), its first CTA, its pieces
+        int found = -1, slot = 0, src, f_first, f_pieces = 1;
+        if (most <= share + kWholeTiles / HEADS) {   // every item whole, in order
+            if (cta >= p.items) return;
+            found = p.split > 1 ? small_div(cta, p.split) : cta;
+            src = rpl > 1 ? small_div(found, rpl) : found;
+            slot = found - src * rpl;
+            f_first = found * p.split;
+        } else {
+            int cap = max(most, 1);
+            // pieces of an item of u tiles: one, or as many as pieces of `cap` tiles take
+            auto pieces_of = [&](int u) { return u <= cap ? 1 : small_div(u + cap - 1, cap); };
+            {   // the smallest of share, 9/8 of it, ... whose pieces find a CTA each
+                for (cap = share; cap < most; cap += (cap + 7) / 8) {
+                    int need = 0;
 #pragma unroll
-                for (int j = 0; j < RPL; ++j) need += un[j] < 0 ? 0 : max((un[j] + cap - 1) / cap, 1);
-                if ((int)__reduce_add_sync(0xffffffffu, need) * p.split <= ctas) break;
+                    for (int j = 0; j < RPL; ++j)
+                        if (j < rpl && un[j] >= 0) need += pieces_of(un[j]);
+                    if ((int)__reduce_add_sync(0xffffffffu, need) * p.split <= ctas) break;
+                }
             }
-        }
-        int mine = 0;
+            int mine = 0, first = 0;
 #pragma unroll
-        for (int j = 0; j < RPL; ++j) mine += un[j] < 0 ? 0 : max((un[j] + cap - 1) / cap, 1);
-        int run = mine;
+            for (int j = 0; j < RPL; ++j)
+                if (j < rpl && un[j] >= 0) mine += pieces_of(un[j]);
+            int run = mine;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int x = __shfl_up_sync(0xffffffffu, run, o);
-            if (lane >= o) run += x;
-        }
-        run -= mine;
-        int found = -1, f_un = 0, f_len = 0, f_off = 0, f_first = 0, f_pieces = 0;
-#pragma unroll
-        for (int j = 0; j < RPL; ++j) {
-            if (un[j] < 0) continue;
-            const int pc = max((un[j] + cap - 1) / cap, 1);
-            if (cta >= run * p.split && cta < (run + pc) * p.split) {
-                found = lane * rpl + j;
-                f_un = un[j]; f_len = len[j]; f_off = off[j]; f_first = run * p.split; f_pieces = pc;
+            for (int o = 1; o < 32; o <<= 1) {
+                const int x = __shfl_up_sync(0xffffffffu, run, o);
+                if (lane >= o) run += x;
             }
-            run += pc;
+            run -= mine;
+#pragma unroll
+            for (int j = 0; j < RPL; ++j) {
+                if (j >= rpl || un[j] < 0) continue;
+                const int pc = pieces_of(un[j]);
+                if (cta >= run * p.split && cta < (run + pc) * p.split) {
+                    found = lane * rpl + j;
+                    slot = j;
+                    first = run * p.split;
+                    f_pieces = pc;
+                }
+                run += pc;
+            }
+            const unsigned who = __ballot_sync(0xffffffffu, found >= 0);
+            if (who == 0) return;
+            src = __ffs(who) - 1;
+            found = __shfl_sync(0xffffffffu, found, src);
+            slot = __shfl_sync(0xffffffffu, slot, src);
+            f_first = __shfl_sync(0xffffffffu, first, src);
+            f_pieces = __shfl_sync(0xffffffffu, f_pieces, src);
         }
-        const unsigned who = __ballot_sync(0xffffffffu, found >= 0);
-        if (who == 0) return;
-        const int src = __ffs(who) - 1;
-        found = __shfl_sync(0xffffffffu, found, src);
-        item_end = __shfl_sync(0xffffffffu, f_un, src);
-        n = __shfl_sync(0xffffffffu, f_len, src);
-        item_off = __shfl_sync(0xffffffffu, f_off, src);
-        f_first = __shfl_sync(0xffffffffu, f_first, src);
-        f_pieces = __shfl_sync(0xffffffffu, f_pieces, src);
-        const int h = (cta - f_first) / f_pieces, piece = (cta - f_first) % f_pieces;
+        item_end = n = item_off = 0;
+#pragma unroll
+        for (int j = 0; j < RPL; ++j)
+            if (j == slot) { item_end = un[j]; n = len[j]; item_off = off[j]; }
+        item_end = __shfl_sync(0xffffffffu, item_end, src);
+        n = __shfl_sync(0xffffffffu, n, src);
+        item_off = __shfl_sync(0xffffffffu, item_off, src);
+        const int h = f_pieces == 1 ? cta - f_first : small_div(cta - f_first, f_pieces), piece = cta - f_first - h * f_pieces;
         item = found * p.split + h;
         c_first = f_first + h * f_pieces;
         c_last = c_first + f_pieces - 1;
@@ -461,9 +491,10 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
                         const bool sets = unset[nt][j] && top > -INFINITY;
-                        const float up = sets ? top : unset[nt][j] ? 0.f : fmaxf(top, 0.f), shrink = sets ? 0.f : fast_exp2(-up);
+                        const float now = ref[nt][j] + (sets ? top : unset[nt][j] ? 0.f : fmaxf(top, 0.f));
+                        const float up = now - ref[nt][j], shrink = sets ? 0.f : fast_exp2(-up);   // (by what the reference really moves)
                         unset[nt][j] = unset[nt][j] && !sets;
-                        ref[nt][j] += up;
+                        ref[nt][j] = now;
 #pragma unroll
                         for (int b = 0; b < kBlocks; ++b) {
                             x[b][nt][j] -= up;
@@ -765,6 +796,7 @@ int launch_decode_quantized(const aircache_shape_t *s, const aircache_quantized_
     p.row_heads = row_heads_of(s);
     p.G = s->n_q_heads / s->n_kv_heads;
     p.items = (int)n_cells(s);
+    p.n_regions = p.items;
     p.split = 1;
     p.sl2 = s->scale * kLog2e;
     int heads = p.row_heads;

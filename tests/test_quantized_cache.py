@@ -238,6 +238,7 @@ LENGTHS = {
     "edges": [0, 1, 15, 16, 17, 63, 64, 65, 0, 127, 128, 129, 300],
     "long": [5000, 3],
     "many": [(7 * i) % 50 for i in range(200)],
+    "lanes": [(37 * i) % 90 + (4000 if i == 41 else 0) for i in range(100)],   # more than a warp's lanes, one far longer
     "most": [(5 * i) % 40 for i in range(1792)],   # as many regions as a shape may have
 }
 
@@ -290,7 +291,7 @@ def test_quantize_leaves_out_regions_that_do_not_fit():
 @pytest.mark.gpu
 @pytest.mark.parametrize("H,G,d", [(1, 7, 128), (2, 4, 64), (4, 7, 128), (4, 16, 64), (8, 8, 128), (2, 16, 128), (8, 9, 128),
                                    (1, 1, 64), (8, 2, 64), (1, 12, 64)])
-@pytest.mark.parametrize("lens", ["one", "edges", "long", "many"])
+@pytest.mark.parametrize("lens", ["one", "edges", "long", "many", "lanes"])
 def test_decode(lens, H, G, d):
     c = Cache(LENGTHS[lens], H, d, Hq=H * G, slack=1, seed=G)
     want = c.expected()
@@ -336,6 +337,24 @@ def test_decode_sharp_and_wide_values():
     out = torch.full(q.shape, float("nan"), device=DEV)
     ac.aircache_decode_attn_quantized(c.sh, c.cache8, q, out, c.ws)
     c.check_attention(q, out, want, c.lens0)
+
+
+@pytest.mark.gpu
+def test_decode_keys_without_a_finite_logit_first():
+    """The first rows of a region have logits of minus infinity (their scale times the query leaves fp32); what follows counts."""
+    c = Cache([300, 40], 2, 64, Hq=8, seed=8)
+    ac.aircache_quantize(c.sh, c.ragged, c.cache8)
+    q = queries(c, 4)
+    q[0, :4] = q[0, :4].abs() + 1
+    c.k8[:64, 0] = 0xfe                                # -448
+    c.k_scale[0, 0] = 2.0 ** 120
+    want = {x: getattr(c, x).cpu().numpy() for x in ("k8", "v8", "k_scale", "v_scale")}
+    out = torch.full((2, 8, 64), float("nan"), device=DEV)
+    ac.aircache_decode_attn_quantized(c.sh, c.cache8, q, out, c.ws)
+    k, v, held = c.values(want, [300, 40])[0]
+    for h in range(4):   # without the first block
+        ref, tol = attention(q[0, h:h + 1].double().cpu().numpy(), k[64:, 0], v[64:, 0], c.sh.scale, held[0])
+        assert (np.abs(out[0, h:h + 1].double().cpu().numpy() - ref) <= tol).all()
 
 
 @pytest.mark.gpu
