@@ -520,58 +520,84 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
                         for (int i = 0; i < 4; ++i) acc[nt][c][i] *= shrink;
             }
             const float vf = v_scale * v_inv;
+            // Both blocks of a tile at a time, or one (9 to 16 heads: the registers).
+            constexpr int GROUP = NT == 2 ? 1 : kBlocks;
+            constexpr bool DIRECT = NT == 2 && D == 128;
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) {
-                uint32_t head_b[NT][2], rest_b[NT][2];
+            for (int b0 = 0; b0 < kBlocks; b0 += GROUP) {
+                uint32_t head_b[GROUP][NT][2], rest_b[GROUP][NT][2], vw[GROUP][4][C::MT / 2];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (int b = 0; b < GROUP; ++b) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {   // keys g (i = 0) and g + 8
-                        const float p0 = fast_exp2(x[b][nt][2 * i]), p1 = fast_exp2(x[b][nt][2 * i + 1]);
-                        sum[nt][0] += p0;
-                        sum[nt][1] += p1;
-                        const uint32_t hi = f16x2(p0 * vf, p1 * vf);
-                        const float2 back = f16x2_f32(hi);
-                        head_b[nt][i] = movmatrix_trans(hi);
-                        rest_b[nt][i] = movmatrix_trans(f16x2(fmaf(p0, vf, -back.x), fmaf(p1, vf, -back.y)));
-                    }
-                const unsigned char *v_tile = tile + C::HALF + b * 16 * D;
-                uint32_t vw[4][C::MT / 2];
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int key = 2 * t + (i & 1) + 8 * (i >> 1);
-                    if (D == 128) {
-                        const uint4 x4 = *reinterpret_cast<const uint4 *>(v_tile + key * 128 + ((g ^ key) & 7) * 16);
-                        vw[i][0] = x4.x; vw[i][1] = x4.y; vw[i][C::MT / 2 - 2] = x4.z; vw[i][C::MT / 2 - 1] = x4.w;
-                    } else {
-                        const uint2 x2 = *reinterpret_cast<const uint2 *>(v_tile + key * 64 + (((g >> 1) ^ (key >> 1)) & 3) * 16 + (g & 1) * 8);
-                        vw[i][0] = x2.x; vw[i][1] = x2.y;
-                    }
-                }
-                if (rows < kTile) {   // behind the rows in use: whatever lies there
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (16 * b + 2 * t + (i & 1) + 8 * (i >> 1) >= rows) {
-#pragma unroll
-                            for (int w = 0; w < C::MT / 2; ++w) vw[i][w] = 0;
+                        for (int i = 0; i < 2; ++i) {   // keys g (i = 0) and g + 8
+                            const float p0 = fast_exp2(x[b0 + b][nt][2 * i]), p1 = fast_exp2(x[b0 + b][nt][2 * i + 1]);
+                            sum[nt][0] += p0;
+                            sum[nt][1] += p1;
+                            const uint32_t hi = f16x2(p0 * vf, p1 * vf);
+                            const float2 back = f16x2_f32(hi);
+                            head_b[b][nt][i] = movmatrix_trans(hi);
+                            rest_b[b][nt][i] = movmatrix_trans(f16x2(fmaf(p0, vf, -back.x), fmaf(p1, vf, -back.y)));
                         }
+                    const unsigned char *v_tile = tile + C::HALF + (b0 + b) * 16 * D;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = 2 * t + (i & 1) + 8 * (i >> 1);
+                        if (D == 128) {
+                            const uint4 x4 = *reinterpret_cast<const uint4 *>(v_tile + key * 128 + ((g ^ key) & 7) * 16);
+                            vw[b][i][0] = x4.x; vw[b][i][1] = x4.y; vw[b][i][C::MT / 2 - 2] = x4.z; vw[b][i][C::MT / 2 - 1] = x4.w;
+                        } else {
+                            const uint2 x2 = *reinterpret_cast<const uint2 *>(v_tile + key * 64 + (((g >> 1) ^ (key >> 1)) & 3) * 16 + (g & 1) * 8);
+                            vw[b][i][0] = x2.x; vw[b][i][1] = x2.y;
+                        }
+                    }
+                    if (rows < kTile) {   // behind the rows in use: whatever lies there
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (16 * (b0 + b) + 2 * t + (i & 1) + 8 * (i >> 1) >= rows) {
+#pragma unroll
+                                for (int w = 0; w < C::MT / 2; ++w) vw[b][i][w] = 0;
+                            }
+                    }
                 }
+                // The products of a tile are summed from zero and added to the sums by the FMA pipe: the tensor core cuts off what an
+                // addition leaves beyond 24 bits, and over hundreds of rows of one warp that adds up (4300 rows: 6.3e-6 of the
+                // output, 2.7e-7 this way; 184 -> 188 us for a batch of 64).  With 9 to 16 heads of 128 channels there are no registers for
+                // it (two KV heads, 1200 rows: 44 us straight into the sums and 1.7e-6 off, 54 us with 250 bytes of spills).
 #pragma unroll
                 for (int w = 0; w < C::MT / 2; ++w) {
-                    // channels 4w..4w+3 of this lane's stretch, two keys abreast
-                    const uint32_t l01 = __byte_perm(vw[0][w], vw[1][w], 0x5140), u01 = __byte_perm(vw[0][w], vw[1][w], 0x7362);
-                    const uint32_t l23 = __byte_perm(vw[2][w], vw[3][w], 0x5140), u23 = __byte_perm(vw[2][w], vw[3][w], 0x7362);
-                    const uint32_t a0 = e4m3x2_f16x2(l01 & 0xffffu), a1 = e4m3x2_f16x2(l01 >> 16);
-                    const uint32_t a2 = e4m3x2_f16x2(l23 & 0xffffu), a3 = e4m3x2_f16x2(l23 >> 16);
-                    const uint32_t b0 = e4m3x2_f16x2(u01 & 0xffffu), b1 = e4m3x2_f16x2(u01 >> 16);
-                    const uint32_t b2 = e4m3x2_f16x2(u23 & 0xffffu), b3 = e4m3x2_f16x2(u23 >> 16);
+                    float low[NT][4], high[NT][4];   // channel tiles 2w and 2w + 1
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        mma_f16_16816(acc[nt][2 * w], a0, a1, a2, a3, head_b[nt][0], head_b[nt][1]);
-                        mma_f16_16816(acc[nt][2 * w + 1], b0, b1, b2, b3, head_b[nt][0], head_b[nt][1]);
-                        mma_f16_16816(acc[nt][2 * w], a0, a1, a2, a3, rest_b[nt][0], rest_b[nt][1]);
-                        mma_f16_16816(acc[nt][2 * w + 1], b0, b1, b2, b3, rest_b[nt][0], rest_b[nt][1]);
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) low[nt][i] = high[nt][i] = 0.f;
+#pragma unroll
+                    for (int b = 0; b < GROUP; ++b) {
+                        // channels 4w..4w+3 of this lane's stretch, two keys abreast
+                        const uint32_t l01 = __byte_perm(vw[b][0][w], vw[b][1][w], 0x5140), u01 = __byte_perm(vw[b][0][w], vw[b][1][w], 0x7362);
+                        const uint32_t l23 = __byte_perm(vw[b][2][w], vw[b][3][w], 0x5140), u23 = __byte_perm(vw[b][2][w], vw[b][3][w], 0x7362);
+                        const uint32_t a0 = e4m3x2_f16x2(l01 & 0xffffu), a1 = e4m3x2_f16x2(l01 >> 16);
+                        const uint32_t a2 = e4m3x2_f16x2(l23 & 0xffffu), a3 = e4m3x2_f16x2(l23 >> 16);
+                        const uint32_t c0 = e4m3x2_f16x2(u01 & 0xffffu), c1 = e4m3x2_f16x2(u01 >> 16);
+                        const uint32_t c2 = e4m3x2_f16x2(u23 & 0xffffu), c3 = e4m3x2_f16x2(u23 >> 16);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            float(&lo)[4] = DIRECT ? acc[nt][2 * w] : low[nt], (&hi)[4] = DIRECT ? acc[nt][2 * w + 1] : high[nt];
+                        mma_f16_16816(lo, a0, a1, a2, a3, rest_b[b][nt][0], rest_b[b][nt][1]);
+                            mma_f16_16816(hi, c0, c1, c2, c3, rest_b[b][nt][0], rest_b[b][nt][1]);
+                            mma_f16_16816(lo, a0, a1, a2, a3, head_b[b][nt][0], head_b[b][nt][1]);
+                            mma_f16_16816(hi, c0, c1, c2, c3, head_b[b][nt][0], head_b[b][nt][1]);
+                        }
                     }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (DIRECT) continue;
+                        acc[nt][2 * w][i] += low[nt][i];
+                            acc[nt][2 * w + 1][i] += high[nt][i];
+                        }
                 }
             }
             __syncwarp();   // (the stage may be refilled from the next tile on)
