@@ -27,7 +27,8 @@
  * Streams.    All work is enqueued on `cuda_stream` (a cudaStream_t passed as
  *             void*, NULL = the legacy default stream).  No entry point
  *             synchronises or copies device memory to the host, except
- *             aircache_check_status() and aircache_pipeline_host().
+ *             aircache_check_status(), aircache_prompt_check_status() and
+ *             aircache_pipeline_host().
  * Errors.     Return value 0 = success, negative = an AIRCACHE_ERR_* code.  All
  *             argument checks run on the host before anything is launched, so a
  *             failing call has enqueued nothing (aircache_pipeline_host, which
@@ -39,7 +40,8 @@
  *             clusters of the scoring kernels that it holds at once, per
  *             context the kernels' shared-memory limits and the address of
  *             the built-in array of aircache_decode_attn_static (so that a
- *             program may go on after cudaDeviceReset).  All of it may be used
+ *             program may go on after cudaDeviceReset), and per device the
+ *             status word that aircache_prompt_check_status() reads.  All of it may be used
  *             from several threads; calls that share a workspace must be
  *             ordered on one stream.
  * Determinism. Same inputs give the same output bits on every run.
@@ -408,7 +410,9 @@ typedef struct {
  * Rows in front of the first and behind the last sequence stay as they are (NaN
  * there and in other sequences reach nothing).  Within a sequence a value
  * row that is not finite also reaches the tokens up to 255 before it, which it
- * is masked for.  A key of minus infinity in a logit counts as masked.
+ * is masked for.  A key whose logit is minus infinity counts as masked.  Sums are
+ * held in fp32 above a reference that may lie 2^16 below the row's largest weight:
+ * values beyond some 2^100 may overflow them.
  */
 int aircache_prompt_attn(const aircache_prompt_t *spec, const aircache_tokens_t *q, const aircache_tokens_t *k,
                          const aircache_tokens_t *v, const int32_t *q_offsets, const int32_t *k_offsets,
@@ -480,10 +484,14 @@ int aircache_append_quantized(const aircache_shape_t *shape, aircache_quantized_
  * aircache_decode_attn over the cache of 8 bits:  out_h = sum_j
  * softmax_j(scale * <q_h, k_g[j]>) * v_g[j] with the elements' values, bf16
  * queries, fp32 accumulation, fp32 output.  A region with lens[r] = 0 yields
- * zeros, and so does one whose rows leave the buffers.  The weights enter the second product as an fp16 head
- * and an fp16 remainder (2^-22), below 2^-36 of the largest weight times the
- * largest scale seen they vanish.  No wait in the kernel depends on another
- * block.
+ * zeros, and so does one whose rows leave the buffers (lens[r] beyond
+ * offsets[r+1] - offsets[r] counts as that).  The weights enter the second
+ * product as an fp16 head and an fp16 remainder (2^-22); below 2^-36 of the
+ * largest weight times the region's largest V scale they vanish.  Off by some
+ * 3e-7 of the output (9 to 16 query heads of 128 channels to a KV head: 1e-5
+ * over thousands of rows).  Device-side waits are bounded; if one gives up,
+ * aircache_check_status() reports AIRCACHE_ERR_TIMEOUT.  Uses the workspace's
+ * status word, tickets and partial slots, as aircache_decode_attn does.
  */
 int aircache_decode_attn_quantized(const aircache_shape_t *shape, const aircache_quantized_t *cache, const void *q,
                                    float *out, void *workspace, int64_t workspace_bytes, void *cuda_stream);
