@@ -412,7 +412,9 @@ typedef struct {
  * row that is not finite also reaches the tokens up to 255 before it, which it
  * is masked for.  A key whose logit is minus infinity counts as masked.  Sums are
  * held in fp32 above a reference that may lie 2^16 below the row's largest weight:
- * values beyond some 2^100 may overflow them.
+ * values beyond some 2^100 may overflow them.  Strides that no tensor map
+ * describes (2^40 bytes or more) are AIRCACHE_ERR_UNSUPPORTED; a stride of 0
+ * (heads that are one and the same) is taken for k and v.
  */
 int aircache_prompt_attn(const aircache_prompt_t *spec, const aircache_tokens_t *q, const aircache_tokens_t *k,
                          const aircache_tokens_t *v, const int32_t *q_offsets, const int32_t *k_offsets,
@@ -462,7 +464,7 @@ int64_t aircache_scale_blocks(const aircache_shape_t *shape, int64_t total_rows,
  * x is held as the e4m3 number nearest to x / s (ties to even).  Infinities
  * become +-448 s, NaN stays NaN.  Slack rows, and the scales of blocks that hold
  * none in use, stay as they are.  out->offsets and out->lens must be the arrays of
- * `cache`.  A region whose rows leave either buffer is left out; lens[r] beyond
+ * `cache`; out->k and out->v must not overlap its k and v.  A region whose rows leave either buffer is left out; lens[r] beyond
  * offsets[r+1] - offsets[r] counts as that.
  */
 int aircache_quantize(const aircache_shape_t *shape, const aircache_ragged_t *cache, aircache_quantized_t *out,

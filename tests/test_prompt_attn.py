@@ -211,6 +211,32 @@ def test_captured_two_streams_and_same_bits():
 
 
 @pytest.mark.gpu
+def test_beside_the_scores_of_another_stream():
+    """The scoring kernel has tensor memory and clusters of its own; calls of both on two streams leave each other alone."""
+    L, B, Hq, Hkv, d, Nv, Nt = 4, 2, 28, 4, 128, 2000, 64
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    s = Session(ac.shape(L, B, Hq, Hkv, d, Nv, Nt, 16), 0.2, device=DEV)
+    k = torch.randn((L, B, Nv + Nt, Hkv, d), generator=gen, device=DEV).bfloat16()
+    s.set_full(k.permute(0, 1, 3, 2, 4), k.permute(0, 1, 3, 2, 4))
+    qw = torch.randn((L, B, 16, Hq, d), generator=gen, device=DEV).bfloat16()
+    s.score(qw)
+    scores = s.scores.clone()
+    n = [900, 300, 41]
+    x = inputs(sum(n), sum(n), Hq, Hkv, d, seed=4)
+    want = attend(*x, n, n)
+    out, off = torch.zeros_like(want), offsets(n)
+    spec, views = ac.prompt(3, sum(n), sum(n), Hq, Hkv, d), [ac.tokens_view(t) for t in x]
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(30):
+        ac.aircache_prompt_attn(spec, *views, off, None, ac.tokens_view(out), stream=a)
+        s.score(qw, stream=b)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(s.scores, scores)
+    assert s.status() == 0 and ac.aircache_prompt_check_status() == 0
+
+
+@pytest.mark.gpu
 def test_from_the_projection_to_decoding():
     """A layer after the other as an engine runs them: rotation into the cache, attention over it, scores, then the
     compression, 8 bits, and a token.  Two sequences of 300 visual and 20 text tokens."""
