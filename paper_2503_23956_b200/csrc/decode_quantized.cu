@@ -27,6 +27,11 @@
 // Numbers.  q is scaled by a power of two per head, so that its largest magnitude is 2^7 to 2^8 in fp16: what is 2^-32 of it is lost.
 // The reference of the softmax follows the largest logit lazily (it moves when one is more than 2^4 above), p <= 2^4.  p
 // times its block's V scale over the largest V scale seen, times 2^11, is split into an fp16 head and remainder (22 bits).  Sums in fp32.
+//
+// Measured (one B200, us a call; bytes at 6.54 TB/s in brackets): 64 sequences of 548 rows in 28 layers, 28 / 4 heads of 128: 188 [160], 207 to 212
+// in a second of calls back to back under the power cap; 640 cells of one KV head 80 [61]; one image 11.9 [3.9], four videos 38.6 [20.4].  A tile takes a
+// warp some 2270 cycles, the memory's rate leaves it 2700: conversions, 2 x 24 products and the softmax, 500 instructions.  16 warps of
+// 16-row tiles: 221 us for the 184 that this took then; items of one head for many regions: 43 for 37.
 #include <cuda.h>
 
 #include <atomic>
@@ -105,7 +110,9 @@ struct DecodeQCfg {
     static_assert(SMEM <= 232448 - 2048, "shared memory of a block");
 };
 
-constexpr int kWholeTiles = 32;   // an item stays whole up to this many tiles (by warps) above the equal share
+// An item stays whole up to this many tiles (of one head's warps) above the equal share: one image, 112 items of 27 tiles on
+// average, 11.7 us whole and 15.6 with the longest ones cut (a merge takes as long as some 30 tiles).
+constexpr int kWholeTiles = 32;
 
 // a / b for a >= 0, b > 0, through the fp32 divider when both are below 2^23 (an integer division by a run-time divisor costs
 // some hundred cycles of the plan)
