@@ -489,9 +489,9 @@ int aircache_append_quantized(const aircache_shape_t *shape, aircache_quantized_
  * zeros, and so does one whose rows leave the buffers (lens[r] beyond
  * offsets[r+1] - offsets[r] counts as that).  The weights enter the second
  * product as an fp16 head and an fp16 remainder (2^-22); below 2^-36 of the
- * largest weight times the region's largest V scale (2^-116 at least) they vanish.  Off by some
- * 3e-7 of the output (9 to 16 query heads of 128 channels to a KV head: 1e-5
- * over thousands of rows).  Device-side waits are bounded; if one gives up,
+ * largest weight times the region's largest V scale (2^-116 at least) they
+ * vanish.  Off by some 3e-7 of the output, whatever the number of rows.
+ * Device-side waits are bounded; if one gives up,
  * aircache_check_status() reports AIRCACHE_ERR_TIMEOUT.  Uses the workspace's
  * status word, tickets and partial slots, as aircache_decode_attn does.
  */

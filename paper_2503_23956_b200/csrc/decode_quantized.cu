@@ -91,6 +91,14 @@ __device__ __forceinline__ float2 f16x2_f32(uint32_t h) {
     return r;
 }
 
+// 16 bytes of shared memory, not asked for ahead of where the program has them (volatile): with 9 to 16 heads of 128 channels
+// there are no registers for more of them at a time
+__device__ __forceinline__ uint4 lds16(const void *from) {
+    uint4 x;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(smem_u32(from)));
+    return x;
+}
+
 // the warps of one KV head
 __device__ __forceinline__ void head_barrier(int head, int threads) {
     asm volatile("bar.sync %0, %1;" ::"r"(head + 1), "r"(threads) : "memory");
@@ -533,7 +541,6 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
             const float vf = v_scale * v_inv;
             // Both blocks of a tile at a time, or one (9 to 16 heads: the registers).
             constexpr int GROUP = NT == 2 ? 1 : kBlocks;
-            constexpr bool DIRECT = NT == 2 && D == 128;
 #pragma unroll
             for (int b0 = 0; b0 < kBlocks; b0 += GROUP) {
                 uint32_t head_b[GROUP][NT][2], rest_b[GROUP][NT][2], vw[GROUP][4][C::MT / 2];
@@ -556,7 +563,8 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
                     for (int i = 0; i < 4; ++i) {
                         const int key = 2 * t + (i & 1) + 8 * (i >> 1);
                         if (D == 128) {
-                            const uint4 x4 = *reinterpret_cast<const uint4 *>(v_tile + key * 128 + ((g ^ key) & 7) * 16);
+                            const unsigned char *from = v_tile + key * 128 + ((g ^ key) & 7) * 16;
+                            const uint4 x4 = NT == 2 ? lds16(from) : *reinterpret_cast<const uint4 *>(from);
                             vw[b][i][0] = x4.x; vw[b][i][1] = x4.y; vw[b][i][C::MT / 2 - 2] = x4.z; vw[b][i][C::MT / 2 - 1] = x4.w;
                         } else {
                             const uint2 x2 = *reinterpret_cast<const uint2 *>(v_tile + key * 64 + (((g >> 1) ^ (key >> 1)) & 3) * 16 + (g & 1) * 8);
@@ -574,41 +582,44 @@ decode_quantized_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_c
                 }
                 // The products of a tile are summed from zero and added to the sums by the FMA pipe: the tensor core cuts off what an
                 // addition leaves beyond 24 bits, and over hundreds of rows of one warp that adds up (4300 rows: 6.3e-6 of the
-                // output, 2.7e-7 this way; 184 -> 188 us for a batch of 64).  With 9 to 16 heads of 128 channels there are no registers for
-                // it (two KV heads, 1200 rows: 44 us straight into the sums and 1.7e-6 off, 54 us with 250 bytes of spills).
+                // output, 2.7e-7 this way; 184 -> 188 us for a batch of 64; with 16 heads to each of two KV heads and some 150 bytes of
+                // spills, eight sequences of 1139 rows 44.3 -> 49.8, 32 of them 124 -> 139).
 #pragma unroll
                 for (int w = 0; w < C::MT / 2; ++w) {
-                    float low[NT][4], high[NT][4];   // channel tiles 2w and 2w + 1
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) low[nt][i] = high[nt][i] = 0.f;
+                    uint32_t a[GROUP][8];   // channels 4w..4w+3 of this lane's stretch, two keys abreast
 #pragma unroll
                     for (int b = 0; b < GROUP; ++b) {
-                        // channels 4w..4w+3 of this lane's stretch, two keys abreast
                         const uint32_t l01 = __byte_perm(vw[b][0][w], vw[b][1][w], 0x5140), u01 = __byte_perm(vw[b][0][w], vw[b][1][w], 0x7362);
                         const uint32_t l23 = __byte_perm(vw[b][2][w], vw[b][3][w], 0x5140), u23 = __byte_perm(vw[b][2][w], vw[b][3][w], 0x7362);
-                        const uint32_t a0 = e4m3x2_f16x2(l01 & 0xffffu), a1 = e4m3x2_f16x2(l01 >> 16);
-                        const uint32_t a2 = e4m3x2_f16x2(l23 & 0xffffu), a3 = e4m3x2_f16x2(l23 >> 16);
-                        const uint32_t c0 = e4m3x2_f16x2(u01 & 0xffffu), c1 = e4m3x2_f16x2(u01 >> 16);
-                        const uint32_t c2 = e4m3x2_f16x2(u23 & 0xffffu), c3 = e4m3x2_f16x2(u23 >> 16);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            float(&lo)[4] = DIRECT ? acc[nt][2 * w] : low[nt], (&hi)[4] = DIRECT ? acc[nt][2 * w + 1] : high[nt];
-                        mma_f16_16816(lo, a0, a1, a2, a3, rest_b[b][nt][0], rest_b[b][nt][1]);
-                            mma_f16_16816(hi, c0, c1, c2, c3, rest_b[b][nt][0], rest_b[b][nt][1]);
-                            mma_f16_16816(lo, a0, a1, a2, a3, head_b[b][nt][0], head_b[b][nt][1]);
-                            mma_f16_16816(hi, c0, c1, c2, c3, head_b[b][nt][0], head_b[b][nt][1]);
-                        }
+                        a[b][0] = e4m3x2_f16x2(l01 & 0xffffu);
+                        a[b][1] = e4m3x2_f16x2(l01 >> 16);
+                        a[b][2] = e4m3x2_f16x2(l23 & 0xffffu);
+                        a[b][3] = e4m3x2_f16x2(l23 >> 16);
+                        a[b][4] = e4m3x2_f16x2(u01 & 0xffffu);
+                        a[b][5] = e4m3x2_f16x2(u01 >> 16);
+                        a[b][6] = e4m3x2_f16x2(u23 & 0xffffu);
+                        a[b][7] = e4m3x2_f16x2(u23 >> 16);
                     }
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int nt = 0; nt < NT; ++nt) {
+                        float low[4] = {0.f, 0.f, 0.f, 0.f}, high[4] = {0.f, 0.f, 0.f, 0.f};   // channel tiles 2w and 2w + 1
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            if (DIRECT) continue;
-                        acc[nt][2 * w][i] += low[nt][i];
-                            acc[nt][2 * w + 1][i] += high[nt][i];
+                        for (int b = 0; b < GROUP; ++b) {
+                            mma_f16_16816(low, a[b][0], a[b][1], a[b][2], a[b][3], rest_b[b][nt][0], rest_b[b][nt][1]);
+                            mma_f16_16816(high, a[b][4], a[b][5], a[b][6], a[b][7], rest_b[b][nt][0], rest_b[b][nt][1]);
+                            mma_f16_16816(low, a[b][0], a[b][1], a[b][2], a[b][3], head_b[b][nt][0], head_b[b][nt][1]);
+                            mma_f16_16816(high, a[b][4], a[b][5], a[b][6], a[b][7], head_b[b][nt][0], head_b[b][nt][1]);
                         }
+#pragma unroll
+                        for (int i = 0; i < 4; i += 2) {
+                            const float2 l = add2(make_float2(acc[nt][2 * w][i], acc[nt][2 * w][i + 1]), make_float2(low[i], low[i + 1]));
+                            const float2 h = add2(make_float2(acc[nt][2 * w + 1][i], acc[nt][2 * w + 1][i + 1]), make_float2(high[i], high[i + 1]));
+                            acc[nt][2 * w][i] = l.x;
+                            acc[nt][2 * w][i + 1] = l.y;
+                            acc[nt][2 * w + 1][i] = h.x;
+                            acc[nt][2 * w + 1][i + 1] = h.y;
+                        }
+                    }
                 }
             }
             __syncwarp();   // (the stage may be refilled from the next tile on)
