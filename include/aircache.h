@@ -41,7 +41,8 @@
  *             context the kernels' shared-memory limits and the address of
  *             the built-in array of aircache_decode_attn_static (so that a
  *             program may go on after cudaDeviceReset), and per device the
- *             status word that aircache_prompt_check_status() reads.  All of it may be used
+ *             count that aircache_prompt_check_status() reads, with what each
+ *             stream has seen of it.  All of it may be used
  *             from several threads; calls that share a workspace must be
  *             ordered on one stream.
  * Determinism. Same inputs give the same output bits on every run.
@@ -422,9 +423,12 @@ int aircache_prompt_attn(const aircache_prompt_t *spec, const aircache_tokens_t 
 
 /*
  * Synchronises the stream and returns 0, or AIRCACHE_ERR_TIMEOUT if a bounded
- * wait in aircache_prompt_attn gave up on the current device since the last call
- * (a wait there is for the block's own copies and products; out is then
- * incomplete).  Not to be called during a stream capture.
+ * wait in aircache_prompt_attn gave up on the current device since this stream
+ * was last checked (the first time: since the context was made).  A wait there is
+ * for the block's own copies and products; out is then incomplete.  Which stream
+ * the call was on is not told apart: a failure is reported to every stream that
+ * is checked, and a check of one takes nothing from the others.  Not to be called
+ * during a stream capture.
  */
 int aircache_prompt_check_status(void *cuda_stream);
 
@@ -512,7 +516,7 @@ int aircache_reset_status(void *workspace, int64_t workspace_bytes, void *cuda_s
  * AIRCACHE_ERR_TIMEOUT (a bounded wait gave up) or AIRCACHE_ERR_INCONSISTENT
  * (aircache_compact met values that do not fit the buffers).  The only
  * device-to-host read in the library apart from
- * aircache_pipeline_host().
+ * aircache_prompt_check_status() and aircache_pipeline_host().
  */
 int aircache_check_status(void *workspace, int64_t workspace_bytes, void *cuda_stream);
 
@@ -525,6 +529,12 @@ int aircache_check_status(void *workspace, int64_t workspace_bytes, void *cuda_s
  * clears it.  Shows that a stuck wait ends in an error code, not in a hang.
  */
 int aircache_selftest_wait_timeout(void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
+/*
+ * The same for aircache_prompt_attn: the wait's end is counted as one of that
+ * call's, and aircache_prompt_check_status() reports it.
+ */
+int aircache_selftest_prompt_timeout(void *cuda_stream);
 
 /*
  * 1 if the whole host range [host_ptr, host_ptr + bytes) is page-locked memory

@@ -114,6 +114,7 @@ _SIGNATURES = {
     "aircache_reset_status": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p]),
     "aircache_check_status": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p]),
     "aircache_selftest_wait_timeout": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p]),
+    "aircache_selftest_prompt_timeout": (C.c_int, [C.c_void_p]),
     "aircache_host_range_is_mapped": (C.c_int, [C.c_void_p, C.c_int64]),
     "aircache_pipeline_host": (C.c_int, [C.POINTER(Shape), C.POINTER(Full), C.c_int64, C.c_void_p, C.c_void_p,
                                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_float,
@@ -467,6 +468,13 @@ def aircache_selftest_wait_timeout(workspace, stream=None, check=True) -> int:
     rc = lib().aircache_selftest_wait_timeout(_ptr(workspace), _nbytes(workspace), _stream(stream))
     if check:
         _check("aircache_selftest_wait_timeout", rc)
+    return rc
+
+
+def aircache_selftest_prompt_timeout(stream=None, check=True) -> int:
+    rc = lib().aircache_selftest_prompt_timeout(_stream(stream))
+    if check:
+        _check("aircache_selftest_prompt_timeout", rc)
     return rc
 
 

@@ -493,6 +493,8 @@ int aircache_selftest_wait_timeout(void *workspace, int64_t workspace_bytes, voi
     return launch_selftest_timeout(workspace, (cudaStream_t)cuda_stream);
 }
 
+int aircache_selftest_prompt_timeout(void *cuda_stream) { return launch_prompt_timeout((cudaStream_t)cuda_stream); }
+
 // Device address of a host range if all of it is page-locked memory the GPU can read in place, else null.
 static void *mapped_host_range(const void *p, int64_t bytes) {
     if (!p || bytes < 1) return nullptr;

@@ -177,6 +177,7 @@ int launch_prompt(const aircache_prompt_t *s, const aircache_tokens_t *q, const 
                   const aircache_tokens_t *v, const int32_t *q_offsets, const int32_t *k_offsets,
                   const aircache_tokens_t *out, cudaStream_t st);
 int prompt_status(cudaStream_t st);
+int launch_prompt_timeout(cudaStream_t st);
 int launch_quantize(const aircache_shape_t *s, const aircache_ragged_t *c, aircache_quantized_t *out, cudaStream_t st);
 int launch_append_quantized(const aircache_shape_t *s, aircache_quantized_t *c, const void *k_new, const void *v_new,
                             cudaStream_t st);

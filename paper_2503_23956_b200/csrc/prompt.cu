@@ -37,6 +37,7 @@
 #include <cuda.h>
 
 #include <atomic>
+#include <mutex>
 
 #include "common.cuh"
 #include "ptx.cuh"
@@ -45,7 +46,7 @@ namespace aircache {
 
 namespace {
 
-__device__ uint32_t g_prompt_status;   // set when a bounded wait gave up
+__device__ uint32_t g_prompt_timeouts;   // blocks in which a bounded wait gave up, since the context was made
 
 constexpr int kKeys = 128;             // keys of a tile
 constexpr float kRise = 16.f;          // a row's reference moves when a logit is more than this above it (log2)
@@ -159,6 +160,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     __shared__ Unit s_unit[2];
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_abort;
+    __shared__ uint32_t s_status;   // which wait gave up
     const uint32_t smem = (smem_u32(smem_raw) + 1023) & ~1023u;
     const uint32_t q_smem = smem, ring = smem + 2 * C::TILE;
     const uint32_t bars = smem_u32(s_bars);
@@ -167,7 +169,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                    unit_empty = unit_full + 16, answered = unit_empty + 16, met_all = answered + 8;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int TPT = p.tokens_per_tile;
-    uint32_t *status = &g_prompt_status;
+    uint32_t *status = &s_status;
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (warp == 9) tmem_alloc(smem_u32(&s_tmem), 512);
@@ -577,8 +579,10 @@ prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     // their time (bounded) before the block's memory goes.
     tc_fence_before();
     __syncthreads();
-    if (s_abort && tid == 0)
+    if (s_abort && tid == 0) {
+        atomicAdd(&g_prompt_timeouts, 1);
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+    }
     __syncthreads();
     if (warp == 9) tmem_dealloc(tmem, 512);
 }
@@ -644,15 +648,61 @@ int launch_prompt(const aircache_prompt_t *s, const aircache_tokens_t *q, const 
     return s->head_dim == 64 ? launch_d<64, 2>(tm_q, tm_k, tm_v, p, dev, st) : launch_d<128, 2>(tm_q, tm_k, tm_v, p, dev, st);
 }
 
+// The count on the device only grows.  What a stream has seen of it is kept here, under the ids of its context and its own (a
+// handle may come again): no check takes a failure from another one, and none can get lost between a read and a reset.
+// (More streams than places: the oldest is forgotten, and would be told of a failure a second time.)
+struct Seen { uint64_t context; unsigned long long stream; uint32_t count; };
+
 int prompt_status(cudaStream_t st) {
-    uint32_t word = 0;
-    const uint32_t zero = 0;
-    AIRCACHE_CUDA_TRY(cudaMemcpyFromSymbolAsync(&word, g_prompt_status, sizeof word, 0, cudaMemcpyDeviceToHost, st));
+    static std::mutex lock;
+    static Seen seen[256];
+    static int n = 0, oldest = 0;
+    uint32_t count = 0;
+    unsigned long long id = 0;
+    AIRCACHE_CUDA_TRY(cudaStreamGetId(st, &id));
+    AIRCACHE_CUDA_TRY(cudaMemcpyFromSymbolAsync(&count, g_prompt_timeouts, sizeof count, 0, cudaMemcpyDeviceToHost, st));
     AIRCACHE_CUDA_TRY(cudaStreamSynchronize(st));
-    if (!word) return AIRCACHE_OK;
-    AIRCACHE_CUDA_TRY(cudaMemcpyToSymbolAsync(g_prompt_status, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, st));
-    AIRCACHE_CUDA_TRY(cudaStreamSynchronize(st));
-    return AIRCACHE_ERR_TIMEOUT;
+    const uint64_t context = context_id();
+    const std::lock_guard<std::mutex> hold(lock);
+    int at = 0;
+    while (at < n && (seen[at].context != context || seen[at].stream != id)) ++at;
+    if (at == n) {
+        if (count == 0) return AIRCACHE_OK;
+        if (n < 256) {
+            ++n;
+        } else {
+            at = oldest;
+            oldest = (oldest + 1) % 256;
+        }
+        seen[at] = {context, id, 0};
+    }
+    const bool more = seen[at].count != count;
+    seen[at].count = count;
+    return more ? AIRCACHE_ERR_TIMEOUT : AIRCACHE_OK;
+}
+
+// A wait that nobody ends, counted as one of prompt_kernel's.
+namespace {
+__global__ void prompt_timeout_kernel() {
+    __shared__ uint64_t s_bar;
+    __shared__ volatile int s_abort;
+    __shared__ uint32_t s_status;
+    if (threadIdx.x == 0) {
+        mbar_init(smem_u32(&s_bar), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        s_abort = 0;
+    }
+    __syncthreads();
+    mbar_wait(smem_u32(&s_bar), 0, &s_abort, &s_status, 11);
+    __syncthreads();
+    if (s_abort && threadIdx.x == 0) atomicAdd(&g_prompt_timeouts, 1);
+}
+}  // namespace
+
+int launch_prompt_timeout(cudaStream_t st) {
+    prompt_timeout_kernel<<<1, 64, 0, st>>>();
+    AIRCACHE_LAUNCH_CHECK();
+    return AIRCACHE_OK;
 }
 
 }  // namespace aircache
