@@ -162,10 +162,11 @@ def _per_token_calls():
         except ImportError:
             _native = False
             return _native
-        if _raw_device is None or _raw_stream is None or not hasattr(_binding, "prompt_attn"):   # (an older build's)
+        if _raw_device is None or _raw_stream is None or not hasattr(_binding, "tables"):   # (an older build's)
             _native = False
             return _native
-        _binding.setup(Shape, Ragged, _raw_device, _raw_stream, Tokens, Rotary, Prompt, Quantized)
+        _binding.setup(Shape, Ragged, _raw_device, _raw_stream, Tokens, Rotary, Prompt, Quantized, torch.int32, torch.int64,
+                       torch.float32, torch.bfloat16)
         handle = lib()
         _native = (_binding,) + tuple(C.cast(getattr(handle, name), C.c_void_p).value for name in
                                       ("aircache_decode_attn", "aircache_decode_step", "aircache_decode_attn_quantized",
@@ -182,6 +183,14 @@ def _ptr(t) -> int | None:
     if isinstance(t, int):
         return t
     return t.data_ptr()
+
+
+def _table(name: str, t, *dtypes) -> int | None:
+    """_ptr of a table whose type matters: torch makes 64-bit integers and 32-bit floats where it is not told otherwise."""
+    if isinstance(t, torch.Tensor) and (t.dtype not in dtypes or not t.is_contiguous()):
+        raise TypeError(f"{name}: expected a contiguous tensor of {' or '.join(map(str, dtypes))}, got {t.dtype} with strides "
+                        f"{tuple(t.stride())}")
+    return _ptr(t)
 
 
 def _stream(stream) -> int | None:
@@ -247,11 +256,14 @@ def prompt(n_seqs, q_tokens, k_tokens, n_q_heads, n_kv_heads, head_dim, scale=No
 
 def quantized_view(k, v, k_scale, v_scale, offsets, lens, total_rows: int, first_region: int = 0,
                    scale_blocks: int | None = None) -> Quantized:
-    """`k`, `v`: one byte per element (e4m3 codes).  `scale_blocks` is k_scale's first size where that is a tensor."""
+    """`k`, `v`: one byte per element (e4m3 codes); float32 scales, int64 offsets, int32 lens.  `scale_blocks` is k_scale's first
+    size where that is a tensor."""
     if scale_blocks is None:
         scale_blocks = k_scale.shape[0]
-    return Quantized(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(offsets), _ptr(lens), total_rows,
-                     scale_blocks, first_region)
+    codes = (torch.uint8, torch.int8, torch.float8_e4m3fn)
+    return Quantized(_table("k", k, *codes), _table("v", v, *codes), _table("k_scale", k_scale, torch.float32),
+                     _table("v_scale", v_scale, torch.float32), _table("offsets", offsets, torch.int64),
+                     _table("lens", lens, torch.int32), total_rows, scale_blocks, first_region)
 
 
 # ------------------------------------------------------------------------------------------------
@@ -369,14 +381,16 @@ def aircache_rotate(spec, q, k, v, positions, inv_freq, q_weight, k_weight, q_ou
         try:
             rc = native[0].rotate(native[5], spec, q, k, v, positions, inv_freq, q_weight, k_weight, q_out, k_out, v_out,
                                   rows, n_rows, stream)
-        except TypeError:   # (before the call) perhaps an argument of a kind that only ctypes takes
+        except TypeError:   # (before the call) perhaps an argument of a kind that only ctypes takes; a wrong table is named below
             if not isinstance(spec, Rotary):
                 raise
     if rc is None:
-        rc = lib().aircache_rotate(C.byref(spec), _ref(q), _ref(k), _ref(v), _ptr(positions), _ptr(inv_freq),
-                                   _ptr(q_weight), _ptr(k_weight), _ref(q_out), _ref(k_out), _ref(v_out), _ptr(rows),
-                                   n_rows, _stream(stream))
-    if check:
+        rc = lib().aircache_rotate(C.byref(spec), _ref(q), _ref(k), _ref(v), _table("positions", positions, torch.int32),
+                                   _table("inv_freq", inv_freq, torch.float32),
+                                   _table("q_weight", q_weight, torch.bfloat16),
+                                   _table("k_weight", k_weight, torch.bfloat16), _ref(q_out), _ref(k_out), _ref(v_out),
+                                   _table("rows", rows, torch.int64), n_rows, _stream(stream))
+    if check and rc != OK:
         _check("aircache_rotate", rc)
     return rc
 
@@ -391,8 +405,8 @@ def aircache_prompt_attn(spec, q, k, v, q_offsets, k_offsets, out, stream=None, 
             if not isinstance(spec, Prompt):
                 raise
     if rc is None:
-        rc = lib().aircache_prompt_attn(C.byref(spec), _ref(q), _ref(k), _ref(v), _ptr(q_offsets), _ptr(k_offsets),
-                                        _ref(out), _stream(stream))
+        rc = lib().aircache_prompt_attn(C.byref(spec), _ref(q), _ref(k), _ref(v), _table("q_offsets", q_offsets, torch.int32),
+                                        _table("k_offsets", k_offsets, torch.int32), _ref(out), _stream(stream))
     if check:
         _check("aircache_prompt_attn", rc)
     return rc

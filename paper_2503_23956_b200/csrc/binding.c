@@ -9,7 +9,8 @@
 
 static PyObject *s_shape, *s_ragged, *s_tokens, *s_rotary, *s_prompt, *s_quantized;   /* the binding's structure types */
 static PyObject *s_get_device, *s_get_stream;    /* torch's current device and its current stream's raw handle */
-static PyObject *s_data_ptr, *s_numel, *s_element_size;
+static PyObject *s_int32, *s_int64, *s_float32, *s_bfloat16;   /* torch's types */
+static PyObject *s_data_ptr, *s_numel, *s_element_size, *s_dtype, *s_is_contiguous;
 
 static int struct_address(PyObject *o, PyObject *type, int64_t *w) {
     if (!PyObject_TypeCheck(o, (PyTypeObject *)type)) {
@@ -42,6 +43,30 @@ static int address(PyObject *o, int64_t *w) {
     const int rc = as_int(r, w);
     Py_DECREF(r);
     return rc;
+}
+
+/* The same for a table of one type: a tensor of another one is a TypeError (torch makes 64-bit integers where it is not told
+ * otherwise, and 32-bit positions read from them turn heads by wrong angles).  With `whole` also one with gaps, for tables that
+ * programs cut out of larger ones.  (4 tokens of rotary positions, a call among others: 3.6 us without a look, 3.9 with these,
+ * 4.1 with a look for gaps in all five tables.) */
+static int table(PyObject *o, PyObject *dtype, int whole, int64_t *w) {
+    if (o == Py_None || PyLong_Check(o)) return address(o, w);
+    PyObject *r = PyObject_GetAttr(o, s_dtype);
+    if (!r) {   /* no tensor */
+        if (!PyErr_ExceptionMatches(PyExc_AttributeError)) return -1;
+        PyErr_Clear();
+        return address(o, w);
+    }
+    Py_DECREF(r);   /* (torch keeps its types) */
+    int fits = r == dtype;
+    if (fits && whole) {
+        if (!(r = PyObject_CallMethodNoArgs(o, s_is_contiguous))) return -1;
+        Py_DECREF(r);
+        fits = r == Py_True;
+    }
+    if (fits) return address(o, w);
+    PyErr_SetString(PyExc_TypeError, "a table of another type, or with gaps");
+    return -1;
 }
 
 /* numel() * element_size(); 0 for None and a raw address */
@@ -157,9 +182,10 @@ static PyObject *rotate(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     if (as_int(a[0], &f) || struct_address(a[1], s_rotary, &w[0])) return NULL;
     for (int i = 1; i < 4; ++i)
         if (struct_or_null(a[1 + i], s_tokens, &w[i]) || struct_or_null(a[8 + i], s_tokens, &w[7 + i])) return NULL;
-    for (int i = 4; i < 8; ++i)
-        if (address(a[1 + i], &w[i])) return NULL;
-    if (address(a[12], &w[11]) || as_int(a[13], &w[12]) || stream_handle(a[14], &w[13])) return NULL;
+    if (table(a[5], s_int32, 1, &w[4]) || table(a[6], s_float32, 0, &w[5]) || table(a[7], s_bfloat16, 0, &w[6]) ||
+        table(a[8], s_bfloat16, 0, &w[7]))
+        return NULL;
+    if (table(a[12], s_int64, 1, &w[11]) || as_int(a[13], &w[12]) || stream_handle(a[14], &w[13])) return NULL;
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = ((int (*)(const void *, const void *, const void *, const void *, const void *, const void *, const void *,
@@ -177,8 +203,8 @@ static PyObject *prompt_attn(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     int64_t f, w[8];
     if (n != 9) { PyErr_SetString(PyExc_TypeError, "prompt_attn takes 9 arguments"); return NULL; }
     if (as_int(a[0], &f) || struct_address(a[1], s_prompt, &w[0]) || struct_or_null(a[2], s_tokens, &w[1]) ||
-        struct_or_null(a[3], s_tokens, &w[2]) || struct_or_null(a[4], s_tokens, &w[3]) || address(a[5], &w[4]) ||
-        address(a[6], &w[5]) || struct_or_null(a[7], s_tokens, &w[6]) || stream_handle(a[8], &w[7]))
+        struct_or_null(a[3], s_tokens, &w[2]) || struct_or_null(a[4], s_tokens, &w[3]) ||
+        table(a[5], s_int32, 1, &w[4]) || table(a[6], s_int32, 1, &w[5]) || struct_or_null(a[7], s_tokens, &w[6]) || stream_handle(a[8], &w[7]))
         return NULL;
     int rc;
     Py_BEGIN_ALLOW_THREADS
@@ -189,21 +215,23 @@ static PyObject *prompt_attn(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     return PyLong_FromLong(rc);
 }
 
-/* setup(Shape, Ragged, get_device, get_raw_stream[, Tokens, Rotary, Prompt, Quantized]), once; without the last four, only
- * decode_attn and decode_step may be called */
+/* setup(Shape, Ragged, get_device, get_raw_stream[, Tokens, Rotary, Prompt, Quantized, int32, int64, float32, bfloat16]), once;
+ * without the last eight, only decode_attn and decode_step may be called */
 static PyObject *setup(PyObject *self, PyObject *args) {
     (void)self;
-    PyObject *dev, *stream, *t[6] = {NULL, NULL, NULL, NULL, NULL, NULL};
-    if (!PyArg_ParseTuple(args, "O!O!OO|O!O!O!O!", &PyType_Type, &t[0], &PyType_Type, &t[1], &dev, &stream, &PyType_Type,
-                          &t[2], &PyType_Type, &t[3], &PyType_Type, &t[4], &PyType_Type, &t[5]))
+    PyObject *dev, *stream, *t[6] = {NULL, NULL, NULL, NULL, NULL, NULL}, *d[4] = {NULL, NULL, NULL, NULL};
+    if (!PyArg_ParseTuple(args, "O!O!OO|O!O!O!O!OOOO", &PyType_Type, &t[0], &PyType_Type, &t[1], &dev, &stream, &PyType_Type,
+                          &t[2], &PyType_Type, &t[3], &PyType_Type, &t[4], &PyType_Type, &t[5], &d[0], &d[1], &d[2], &d[3]))
         return NULL;
     Py_INCREF(dev); Py_INCREF(stream);
     for (int i = 0; i < 6; ++i) {
         if (!t[i]) t[i] = (PyObject *)&PyType_Type;   /* no structure is of this type: a TypeError */
         Py_INCREF(t[i]);
     }
+    for (int i = 0; i < 4; ++i) Py_XINCREF(d[i]);
     s_get_device = dev; s_get_stream = stream;
     s_shape = t[0]; s_ragged = t[1]; s_tokens = t[2]; s_rotary = t[3]; s_prompt = t[4]; s_quantized = t[5];
+    s_int32 = d[0]; s_int64 = d[1]; s_float32 = d[2]; s_bfloat16 = d[3];
     Py_RETURN_NONE;
 }
 
@@ -222,6 +250,11 @@ PyMODINIT_FUNC PyInit__binding(void) {
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_numel = PyUnicode_InternFromString("numel");
     s_element_size = PyUnicode_InternFromString("element_size");
-    if (!s_data_ptr || !s_numel || !s_element_size) return NULL;
-    return PyModule_Create(&s_module);
+    s_dtype = PyUnicode_InternFromString("dtype");
+    s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    if (!s_data_ptr || !s_numel || !s_element_size || !s_dtype || !s_is_contiguous) return NULL;
+    PyObject *const tables = PyBool_FromLong(1);   /* says that rotate and prompt_attn look at the types of their tables */
+    PyObject *const module = PyModule_Create(&s_module);
+    if (module && PyModule_AddObject(module, "tables", tables) < 0) { Py_DECREF(module); return NULL; }
+    return module;
 }
