@@ -446,7 +446,9 @@ int aircache_prompt_check_status(void *cuda_stream);
  * scale, a power of two, at [offsets[r] / 64 + first_region + r + j, head] of
  * k_scale and v_scale, f32 [scale_blocks, Hkv]: no two regions share a
  * block, wherever they begin.  An element stands for code * scale.
- * k and v 16-byte aligned.
+ * k and v 16-byte aligned.  Where the 16-bit cache is kept beside it, `lens` is
+ * one array for both: a row appended to one of them is counted in the other,
+ * which does not have it.
  */
 typedef struct {
     void *k, *v;

@@ -40,6 +40,9 @@ class Session:
         self.cache = ragged_view(self.k_c, self.v_c, self.offsets, self.lens, self.rows)
         self.out = torch.empty((L, B, Hq, d), dtype=torch.float32, device=self.dev)
         self.full = None
+        self.cache8 = None
+        self._held8 = False    # the 8-bit cache holds what the last budget() and compact() left, and what was appended since
+        self._grown8 = False   # rows were appended to it: lens counts them, the 16-bit cache does not have them
 
     def set_full(self, k_log: torch.Tensor, v_log: torch.Tensor):
         """k_log, v_log: device bf16 tensors with logical dims [L, B, Hkv, N, d] (any strides, d contiguous)."""
@@ -50,22 +53,36 @@ class Session:
         aircache_score(self.sh, self.full, qw, self.alpha if alpha is None else alpha, self.scores, self.mask,
                        self.ws, stream)
 
+    def _wide(self):
+        if self.k_c is None or self.v_c is None:
+            raise RuntimeError("the 16-bit cache was dropped (k_c and v_c are None)")
+        return self.cache
+
     def budget(self, scores=None, mode=0, stream=None):
         aircache_budget(self.sh, self.scores if scores is None else scores, self.ratio, mode, self.budgets,
                         self.strength, self.skew, self.cache, self.ws, stream)
+        self._held8 = self._grown8 = False   # (new rows and lengths)
 
     def compact(self, scores=None, budgets=None, want_kept=True, stream=None):
         aircache_compact(self.sh, self.full, self.scores if scores is None else scores,
-                         self.budgets if budgets is None else budgets, self.ratio, self.cache,
+                         self.budgets if budgets is None else budgets, self.ratio, self._wide(),
                          self.kept if want_kept else None, self.ws, stream)
+        self._held8 = False
 
     def decode(self, q, out=None, stream=None):
-        aircache_decode_attn(self.sh, self.cache, q, self.out if out is None else out, self.ws, stream)
+        cache = self._wide()
+        if self._grown8:
+            raise RuntimeError("rows were appended in 8 bits, the 16-bit cache does not have them: decode_quantized()")
+        aircache_decode_attn(self.sh, cache, q, self.out if out is None else out, self.ws, stream)
 
     def quantize(self, stream=None):
-        """The compressed cache in 8 bits (self.k8, self.v8, self.k_scale, self.v_scale); its rows and lengths stay those
-        of the 16-bit one, whose k_c and v_c may then be dropped."""
-        if getattr(self, "cache8", None) is None:
+        """The compressed cache in 8 bits (self.k8, self.v8, self.k_scale, self.v_scale).  Its rows and lengths are those of the
+        16-bit one: once append_quantized() has added to them, decode() and quantize() are refused until budget() has set them
+        anew.  Set k_c and v_c to None to give the 16-bit cache's memory back; what needs it is refused from then on."""
+        cache = self._wide()
+        if self._grown8:
+            raise RuntimeError("rows were appended in 8 bits, the 16-bit cache does not have them: budget() and compact() first")
+        if self.cache8 is None:
             blocks = aircache_scale_blocks(self.sh, self.rows)
             self.k8 = torch.empty(self.k_c.shape, dtype=torch.uint8, device=self.dev)
             self.v8 = torch.empty_like(self.k8)
@@ -73,13 +90,20 @@ class Session:
             self.v_scale = torch.empty_like(self.k_scale)
             self.cache8 = quantized_view(self.k8, self.v8, self.k_scale, self.v_scale, self.offsets, self.lens,
                                          self.rows)
-        aircache_quantize(self.sh, self.cache, self.cache8, stream)
+        aircache_quantize(self.sh, cache, self.cache8, stream)
+        self._held8 = True
+
+    def _narrow(self):
+        if not self._held8:
+            raise RuntimeError("the 8-bit cache does not hold the present one: quantize() first")
+        return self.cache8
 
     def append_quantized(self, k_new, v_new, appended, stream=None):
-        aircache_append_quantized(self.sh, self.cache8, k_new, v_new, appended, stream)
+        aircache_append_quantized(self.sh, self._narrow(), k_new, v_new, appended, stream)
+        self._grown8 = True
 
     def decode_quantized(self, q, out=None, stream=None):
-        aircache_decode_attn_quantized(self.sh, self.cache8, q, self.out if out is None else out, self.ws, stream)
+        aircache_decode_attn_quantized(self.sh, self._narrow(), q, self.out if out is None else out, self.ws, stream)
 
     def status(self) -> int:
         return aircache_check_status(self.ws, check=False)
