@@ -28,8 +28,8 @@
 // The reference of the softmax follows the largest logit lazily (it moves when one is more than 2^4 above), p <= 2^4.  p
 // times its block's V scale over the largest V scale seen (2^-116 at least), times 2^11, is split into an fp16 head and remainder (22 bits).  Sums in fp32.
 //
-// Measured (one B200, us a call; bytes at 6.54 TB/s in brackets): 64 sequences of 548 rows in 28 layers, 28 / 4 heads of 128: 188 [160], 207 to 212
-// in a second of calls back to back under the power cap; 640 cells of one KV head 80 [61]; one image 11.9 [3.9], four videos 38.6 [20.4].  A tile takes a
+// Measured (one B200, us a call; bytes at 6.54 TB/s in brackets): 64 sequences of 548 rows in 28 layers, 28 / 4 heads of 128: 189 [160], 207 to 214
+// in a second of calls back to back under the power cap; 640 cells of one KV head 80 [61]; one image 11.9 [3.9], four videos 39.0 [20.4].  A tile takes a
 // warp some 2270 cycles, the memory's rate leaves it 2700: conversions, 2 x 24 products and the softmax, 500 instructions.  16 warps of
 // 16-row tiles: 221 us for the 184 that this took then; items of one head for many regions: 43 for 37.
 #include <cuda.h>

@@ -9,7 +9,8 @@
 // head inside: 128 / G tokens (rounded down) of all G heads, 126 rows at G = 7.  A tile then spans few tokens, which keeps the part
 // that the causal mask throws away small, and a turn of a few tokens still fills rows.  A block takes two such tiles, one behind
 // the other, of one sequence and KV head, and goes over the keys in tiles of 128, all of them once.  Blocks are numbered from the
-// last tokens of the last sequence on: those with the most keys start first; a block that is done takes the work of one that
+// last tokens of the last sequence on, so that within a sequence those with the most keys start first (sequences go by their number,
+// not by their length); a block that is done takes the work of one that
 // has not started (cluster launch control), so that its first copies and products run beside the end of the unit before
 // (9338 tokens and 64 heads: 1327 -> 1245 us when it came).  In calls of so few blocks that each has an SM of its own, a block takes one
 // row tile and its two halves share the key tiles, even and odd; their sums meet in the end.
@@ -22,15 +23,16 @@
 // the product that reads P_i.
 //
 // Measured (one B200, 1662 TFLOP/s by the library's own large products): 9338 tokens, 64 / 8 heads of 128, causal (1429 GFLOP) 1140 to
-// 1170 us a call, 1356 to 1375 in a second of calls back to back, where the power cap holds the clock; eight prompts of 300 to 3172
+// 1190 us a call, 1356 to 1375 in a second of calls back to back, where the power cap holds the clock; eight prompts of 300 to 3172
 // tokens, 28 / 4 heads (95 GFLOP) 132 and 144; 640 tokens of a small model 10.  A step (128 keys, two row tiles) takes 3500 to 3900
 // cycles: its products alone 2900, since a product with A in shared memory takes 106 cycles where its arithmetic takes 64 (A in tensor
 // memory: 75); a row tile's softmax 2500, of which the other tile's products cover most.  Not kept: two threads a row, steps of
 // 64 keys with two score buffers, exponentials as polynomials, the weights handed over in halves (all slower).
 //
 // The reference of a row moves only when a logit is more than 2^16 above it (weights are floating-point numbers: it
-// need not be the maximum); then its warp rescales O_i in tensor memory, behind the last product's commit.  Sums and O_i in fp32.  P is rounded to bf16 (2^-9 of a weight, averaged over
-// the keys, beside 2^-9 of the rounding of the output).
+// need not be the maximum); then its warp rescales O_i in tensor memory, behind the last product's commit.  Sums and O_i in fp32.  P is rounded to bf16 for the second
+// product (up to 2^-8 of a weight, averaged over the keys, beside up to 2^-8 for the rounding of the output; both operands of a product have
+// one type).  Off by 1.2 to 1.4 times what a 32-bit form with the same output is off by.
 //
 // The last key tile of a sequence may hold rows of the next one or of nothing: their logits are masked, and the V rows are
 // zeroed in shared memory before they are multiplied (0 * NaN).
@@ -112,11 +114,6 @@ __device__ __forceinline__ void tmem_ld16_bits(uint32_t taddr, uint32_t (&r)[16]
                  : AIRCACHE_R16("=r", r) : "r"(taddr) : "memory");
 }
 #undef AIRCACHE_R16
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
 
 // 16 columns of tensor memory times `shrink`.
 __device__ __forceinline__ void rescale16(uint32_t at, float shrink) {
@@ -632,8 +629,9 @@ int launch_prompt(const aircache_prompt_t *s, const aircache_tokens_t *q, const 
     p.causal = s->causal;
     p.sl2 = s->scale * kLog2e;
     // One row tile a block, its keys shared by the block's halves, where every block then has an SM of its own: 640 tokens of
-    // a small model 14.0 -> 10.3 us.  In calls of more blocks it reads the keys twice as often (16 turns over some 2000 keys
-    // each, 140 blocks: 51 us with two row tiles, 65 with one).
+    // a small model 14.0 -> 10.3 us.  In calls of more blocks it reads the keys twice as often (16 turns of 1 to 202 tokens
+    // over some 2000 keys each, 116 blocks of two row tiles: 52 us, 65 with one a block).  The count is the host's bound on blocks, a
+    // tile a sequence too many; where most sequences are a token or two, second row tiles are empty (not measured apart).
     const int row_tiles = ((int64_t)s->q_tokens / p.tokens_per_tile + s->n_seqs) * s->n_kv_heads <= sms ? 1 : 2;
     const int64_t units = s->q_tokens / (row_tiles * p.tokens_per_tile) + s->n_seqs;   // at least as many as there are
     if (units * s->n_kv_heads >= ((int64_t)1 << 31)) return AIRCACHE_ERR_UNSUPPORTED;

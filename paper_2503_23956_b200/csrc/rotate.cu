@@ -8,7 +8,7 @@
 // sines a token.  (With 16 consecutive bytes per lane in both layouts, partners fetched by shuffles: 174 us for 27136
 // tokens of 28 + 2 * 4 heads.)  Heads of one token go to one warp where there are many tokens: the angles are
 // then taken once for all of them.  Where there are few, they go to more warps.  27136 tokens, us: 117 with four loads under
-// way and 20 warps an SM, 103 with two and 32 (4.8 TB/s; the norm's sum takes 13 of it, the angles 4).  Measured and not kept: the next
+// way and 20 warps an SM, 103 with two and 32 (4.8 TB/s; the norm's sum takes 13 of it, the angles 4; 64 registers a thread, 3 to 8 of them spilled).  Measured and not kept: the next
 // loads asked for ahead of the angles and of a batch's arithmetic (107), two numbers an instruction (105 to 109), the
 // sums of a batch side by side (109), one load under way and 40 warps (118).
 //
@@ -37,12 +37,6 @@ struct RotateParams {
     int half, sec0, sec01;   // R / 2; frequencies of the first axis, of the first two
     float eps, factor;
 };
-
-__device__ __forceinline__ uint32_t f32_bf16x2(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
 
 template <int D, bool INTERLEAVED>
 __global__ void __launch_bounds__(128, 8) rotate_kernel(RotateParams p) {
@@ -124,8 +118,8 @@ __global__ void __launch_bounds__(128, 8) rotate_kernel(RotateParams p) {
                         }
                     }
                     if (base + b * HPW + sub < to) {
-                        *reinterpret_cast<uint2 *>(dst + 2 * lo) = make_uint2(f32_bf16x2(y[0], y[1]), f32_bf16x2(y[2], y[3]));
-                        *reinterpret_cast<uint2 *>(dst + 2 * hi) = make_uint2(f32_bf16x2(y[4], y[5]), f32_bf16x2(y[6], y[7]));
+                        *reinterpret_cast<uint2 *>(dst + 2 * lo) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+                        *reinterpret_cast<uint2 *>(dst + 2 * hi) = make_uint2(pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
                     }
                     dst += dst_step;
                 }
