@@ -674,8 +674,8 @@ int prompt_status(cudaStream_t st) {
         }
         seen[at] = {context, id, 0};
     }
-    const bool more = seen[at].count != count;
-    seen[at].count = count;
+    const bool more = (int32_t)(count - seen[at].count) > 0;   // (not behind what another thread's check of this stream has read)
+    if (more) seen[at].count = count;
     return more ? AIRCACHE_ERR_TIMEOUT : AIRCACHE_OK;
 }
 
